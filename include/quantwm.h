@@ -315,6 +315,97 @@ size_t quantwm_attend_epochs_workspace_bytes(const quantwm_config* cfg, int32_t 
                                              const int64_t* epoch_start, int64_t n_cache, int64_t n_act,
                                              int64_t n_q);
 
+/* quantwm_attend_epochs with a bounded view of the past: of the keys that the
+ * frame mask shows, a Query sees the first n_sink and the last `window` positions
+ * up to the end of its own frame. With hi(i) = q_start + (i/F + 1) F, key j is
+ * visible iff j < hi(i) and (j < n_sink or j >= hi(i) - window). F = 1 is the
+ * token-causal window (the Query's own position and the window - 1 before it); a
+ * window of W F positions shows the Query's frame and the W - 1 before it; a
+ * window of every position is quantwm_attend_epochs. A Query that sees no key
+ * has O = 0 and lse = -inf. Only the tiles of 64 keys that hold a visible key of a
+ * block of 256 Queries are read, so time and bytes go by n_sink + window, not by
+ * n_cache. n_epochs >= 1 (1: one calibration block, epoch_start may be NULL);
+ * n_act may be 0; n_sink and window are >= 0. Everything else as for
+ * quantwm_attend_epochs, the optional workspace included. */
+quantwm_status quantwm_attend_window(const quantwm_config* cfg, const void* calibs, int32_t n_epochs,
+                                     const int64_t* epoch_start, const void* cache, int64_t n_cache,
+                                     const void* k_act, const void* v_act, int64_t n_act, const void* q,
+                                     int64_t n_q, int64_t q_start, int32_t frame_tokens, int64_t n_sink,
+                                     int64_t window, void* out, float* lse_out, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/* Workspace bytes of quantwm_attend_window's key split (0 where the launch does
+ * not split, or the arguments are invalid). */
+size_t quantwm_attend_window_workspace_bytes(const quantwm_config* cfg, int64_t n_cache, int64_t n_act, int64_t n_q,
+                                             int32_t frame_tokens, int64_t n_sink, int64_t window);
+
+/* Attention of cfg->batch rollouts that branch off one history. Every rollout's
+ * keys are [shared prefix | its own packed keys | its own exact keys], n_prefix +
+ * n_cache + n_act positions: keys [0, n_prefix) come from prefix_cache, a cache of
+ * prefix_cfg (batch 1; heads, head_dim and dtype those of cfg, the rest its own),
+ * appended in n_epochs calibration epochs as in quantwm_attend_epochs; the others
+ * are those of quantwm_attend_active with cfg, calib, cache, k_act and v_act. The
+ * mask is that of quantwm_attend over the concatenated positions; q_start >=
+ * n_prefix, so every Query sees the whole prefix. q, out: [B, n_q, H, d]; lse_out:
+ * optional [B, H, n_q]. The prefix is read and decoded once for the rows of all
+ * rollouts together (they are one chunk of B n_q Queries to it), and its partial
+ * softmax results are joined with those of the own keys by log-sum-exp. n_prefix
+ * and n_cache + n_act may be 0; the pointers of an empty part are not read and may
+ * be NULL. Needs a device workspace of quantwm_attend_shared_workspace_bytes(),
+ * 256-byte aligned (QWM_ERR_INVALID_ARG when it is smaller); calls that share one
+ * must be ordered on one stream, captured graphs included. QWM_ERR_UNSUPPORTED when
+ * B n_q, n_prefix or n_cache + n_act exceeds 0x7fff0000. */
+quantwm_status quantwm_attend_shared(const quantwm_config* prefix_cfg, const void* prefix_calibs, int32_t n_epochs,
+                                     const int64_t* epoch_start, const void* prefix_cache, int64_t n_prefix,
+                                     const quantwm_config* cfg, const void* calib, const void* cache,
+                                     int64_t n_cache, const void* k_act, const void* v_act, int64_t n_act,
+                                     const void* q, int64_t n_q, int64_t q_start, int32_t frame_tokens, void* out,
+                                     float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Device workspace bytes that quantwm_attend_shared needs for these sizes (0 if
+ * the arguments are invalid). They depend on the current device's compute-unit
+ * count. */
+size_t quantwm_attend_shared_workspace_bytes(const quantwm_config* prefix_cfg, int64_t n_prefix,
+                                             const quantwm_config* cfg, int64_t n_cache, int64_t n_act, int64_t n_q);
+
+/* ------------------------------------------------------------ positions */
+
+/* Rotary positions on three axes, for the Queries and Keys of a chunk before they
+ * are appended or attend (append and attention take Keys as they are to be used).
+ * Pair p of a head's channels turns by a = x[axis(p)] * freq[p] radians:
+ *   (u, v) -> (u cos a - v sin a, u sin a + v cos a).
+ * The dims[0]/2 first pairs turn by the token's time, the dims[1]/2 next by its
+ * height, the dims[2]/2 after them by its width; channels past dims[0] + dims[1] +
+ * dims[2] are copied. */
+#define QWM_ROTARY_ADJACENT 0 /* pair p: channels 2 p and 2 p + 1 */
+#define QWM_ROTARY_HALVES 1   /* pair p: channels p and p + (dims[0] + dims[1] + dims[2]) / 2 */
+typedef struct {
+  int32_t pairs;         /* QWM_ROTARY_* */
+  int32_t dims[3];       /* channels of the time, height and width axes: even, summing to at most
+                            head_dim (QWM_ROTARY_HALVES: to a multiple of 16) */
+  int32_t height, width; /* rows and columns of a frame's tokens, for positions from the frame grid */
+  double freq[64];       /* radians per unit of position of every pair */
+} quantwm_rotary_axes;
+
+/* Fills *out with freq = base^(-2 i / D) for pair i of an axis with D channels. */
+quantwm_status quantwm_rotary_init(const quantwm_config* cfg, const int32_t* dims, int32_t height, int32_t width,
+                                   double base, int32_t pairs, quantwm_rotary_axes* out);
+
+/* Turns q and, unless NULL, k by the positions of their tokens. q, k: [B, n, H, d]
+ * with token_stride elements from one token to the next (at least H * d, a multiple
+ * of 16 bytes; heads and channels contiguous, batch entries n * token_stride apart:
+ * a slice of a fused projection, or H * d); q_out, k_out: contiguous [B, n, H, d]. An
+ * output may be its own contiguous input; other overlaps are refused. pos:
+ * optional device int32 [B, n, 3], the tokens' (time, height, width), any values;
+ * NULL takes token i of every batch entry at place pos0 + i of the frame grid: time
+ * (pos0 + i) / (height width), then row and column inside the frame (each below
+ * 2^31). inverse != 0 turns back by the same angles: the transpose of the turn, so
+ * the gradient with respect to its input. Angles are formed in fp64 and the
+ * products in fp32, with one rounding to the element type. n == 0 is a no-op. */
+quantwm_status quantwm_rotary(const quantwm_config* cfg, const quantwm_rotary_axes* axes, int64_t pos0,
+                              const int32_t* pos, const void* q, const void* k, int64_t n, int64_t token_stride,
+                              void* q_out, void* k_out, int32_t inverse, void* stream);
+
 /* For callers that cannot allocate device memory (code under HIP graph capture,
  * tight serving loops, harnesses that forbid hipMalloc): quantwm_attend with
  * no workspace argument. Where quantwm_attend would split the key range

@@ -2,7 +2,7 @@
 
 Translation units compile in parallel: append.hip (fp32) and append_bf16.hip
 once per (head_dim, group size), attend.hip once per (element type, head_dim, PSAC rank padding),
-attend_host.hip, calib.hip, basis.hip, coef.hip and api.hip; the objects link into ``paper_2609_26425_amd/libquantwm.so``.
+attend_host.hip, rotary.hip, calib.hip, basis.hip, coef.hip and api.hip; the objects link into ``paper_2609_26425_amd/libquantwm.so``.
 """
 from __future__ import annotations
 
@@ -46,7 +46,7 @@ def _units():
                               ["-fno-honor-nans", f"-DQWM_ATTEND_T={t}", f"-DQWM_ATTEND_D={d}",
                                f"-DQWM_ATTEND_RP={rp}"]))
     units.append(("attend_host.o", "attend_host.hip", ["-fno-honor-nans"]))
-    for name in ("calib", "basis", "coef", "api"):
+    for name in ("rotary", "calib", "basis", "coef", "api"):
         units.append((f"{name}.o", f"{name}.hip", []))
     return units
 

@@ -463,12 +463,10 @@ size_t quantwm_attend_active_workspace_bytes(const quantwm_config* cfg, int64_t 
   return attend_split_bytes(cfg, n_cache + n_act, n_q, nullptr);
 }
 
-static quantwm_status attend_common(const quantwm_config* cfg, const void* calib, int32_t n_epochs,
-                                    const int64_t* epoch_start, const void* cache, int64_t n_cache,
-                                    const void* k_act, const void* v_act, int64_t n_act, const void* q, int64_t n_q,
-                                    int64_t q_start, int32_t frame_tokens, void* out, float* lse_out,
-                                    float* logits_out, void* workspace, size_t workspace_bytes, void* stream,
-                                    int64_t q_first = 0) {
+// Checks the sizes that every attention form shares (nothing about pointers).
+static quantwm_status check_attend_sizes(const quantwm_config* cfg, int32_t n_epochs, const int64_t* epoch_start,
+                                         int64_t n_cache, int64_t n_act, int64_t n_q, int64_t q_start,
+                                         int32_t frame_tokens) {
   QWM_TRY(check_cfg(cfg));
   if (n_epochs < 1 || n_epochs > qwm::kMaxEpochs) return fail(QWM_ERR_UNSUPPORTED, "n_epochs must be in [1, 64]");
   if (n_epochs > 1) {
@@ -485,6 +483,75 @@ static quantwm_status attend_common(const quantwm_config* cfg, const void* calib
   if (n_act > (int64_t(1) << 26)) return fail(QWM_ERR_UNSUPPORTED, "n_act above 2^26");
   if (q_start > n_cache + n_act) return fail(QWM_ERR_INVALID_ARG, "q_start > n_cache + n_act");
   if (frame_tokens < 1) return fail(QWM_ERR_INVALID_ARG, "frame_tokens must be >= 1");
+  return QWM_OK;
+}
+
+// The argument block of a launch without key split, mask extras and outputs
+// beside out, lse and logits.
+static qwm::AttendArgs attend_args(const quantwm_config* cfg, const void* calib, int32_t n_epochs,
+                                   const int64_t* epoch_start, const void* cache, int64_t n_cache, const void* k_act,
+                                   const void* v_act, int64_t n_act, const void* q, int64_t n_q, int64_t q_start,
+                                   int32_t frame_tokens, void* out, float* lse_out, float* logits_out) {
+  const quantwm_calib_layout C = qwm::calib_layout(*cfg);
+  qwm::AttendArgs a;
+  a.calib = static_cast<const uint8_t*>(calib);
+  a.slab = C.slab_bytes;
+  a.o_mu_k = C.mu_k; a.o_mu_v = C.mu_v; a.o_u_t = C.u_t;
+  a.o_mu_k16 = C.mu_k16; a.o_mu_v16 = C.mu_v16; a.o_e16 = C.e16;
+  a.cache = static_cast<const uint8_t*>(cache);
+  a.L = qwm::cache_layout(*cfg);
+  a.q = q; a.out = out; a.lse = lse_out; a.logits = logits_out;
+  a.n_cache = n_cache; a.n_q = n_q; a.q_start = q_start;
+  a.n_epochs = n_epochs;
+  a.calib_stride = n_epochs > 1 ? int64_t(quantwm_calib_bytes(cfg)) : 0;
+  for (int e = 0; e < qwm::kMaxEpochs; ++e) a.epoch_start[e] = e < n_epochs && n_epochs > 1 ? epoch_start[e] : 0;
+  a.k_act = n_act > 0 ? k_act : nullptr;
+  a.v_act = n_act > 0 ? v_act : nullptr;
+  a.n_act = n_act;
+  a.frame_tokens = frame_tokens; a.heads = cfg->heads; a.n_centroids = cfg->n_centroids; a.rank = cfg->rank;
+  a.tables_in_lds = qwm::attend_tables_fit(cfg->head_dim, qwm::elem_bytes(*cfg), cfg->rank, cfg->n_centroids) ? 1 : 0;
+  a.n_split = 1;
+  a.part_o = nullptr;
+  a.part_ml = nullptr;
+  a.q_row0 = 0;
+  a.windowed = 0;
+  a.n_sink = a.window = 0;
+  return a;
+}
+
+// Gives a launch its partial planes: n_split of them, at `at` of a workspace.
+static void set_planes(const quantwm_config* cfg, qwm::AttendArgs& a, int n_split, void* at) {
+  const size_t rows = size_t(n_split) * cfg->batch * cfg->heads * size_t(a.n_q);
+  a.n_split = n_split;
+  a.part_o = static_cast<float*>(at);
+  a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(at) + (rows * cfg->head_dim * 4 + 255) / 256 * 256);
+}
+
+static hipError_t launch_attend(const quantwm_config* cfg, const qwm::AttendArgs& a, bool logits, hipStream_t s) {
+  return cfg->dtype == QWM_BF16 ? qwm::launch_attend_bf16(a, cfg->head_dim, cfg->batch, logits, s)
+                                : qwm::launch_attend_f32(a, cfg->head_dim, cfg->batch, logits, s);
+}
+
+// Keys that a block of Queries may see under a window (all of them without one):
+// what the key split is chosen for.
+struct Window {
+  int64_t n_sink, window;
+};
+static int64_t keys_in_reach(int64_t n_keys, int32_t frame_tokens, const Window* w) {
+  if (!w) return n_keys;
+  // the window of a block's first row, and the frames that the block's 256 rows span
+  const int64_t F = frame_tokens, span = (256 + F - 1) / F * F;
+  if (w->window > n_keys - span || w->n_sink > n_keys - span - w->window) return n_keys;
+  return w->n_sink + w->window + span;
+}
+
+static quantwm_status attend_common(const quantwm_config* cfg, const void* calib, int32_t n_epochs,
+                                    const int64_t* epoch_start, const void* cache, int64_t n_cache,
+                                    const void* k_act, const void* v_act, int64_t n_act, const void* q, int64_t n_q,
+                                    int64_t q_start, int32_t frame_tokens, void* out, float* lse_out,
+                                    float* logits_out, void* workspace, size_t workspace_bytes, void* stream,
+                                    int64_t q_first = 0, const Window* window = nullptr) {
+  QWM_TRY(check_attend_sizes(cfg, n_epochs, epoch_start, n_cache, n_act, n_q, q_start, frame_tokens));
   if (n_q == 0) return ok();
   QWM_TRY(check_dev(calib, "calib"));
   QWM_TRY(check_dev(cache, "cache"));
@@ -503,41 +570,21 @@ static quantwm_status attend_common(const quantwm_config* cfg, const void* calib
   const bool sparse_rows = (cfg->storage & QWM_STORE_SPARSE) != 0;
   if (sparse_rows && logits_out)
     return fail(QWM_ERR_UNSUPPORTED, "the logits hook reads slot-addressed rows; the cache keeps sparse rows");
-  const int elem = qwm::elem_bytes(*cfg);
-  const bool tables = qwm::attend_tables_fit(cfg->head_dim, elem, cfg->rank, cfg->n_centroids);
-  const quantwm_calib_layout C = qwm::calib_layout(*cfg);
-  qwm::AttendArgs a;
-  a.calib = static_cast<const uint8_t*>(calib);
-  a.slab = C.slab_bytes;
-  a.o_mu_k = C.mu_k; a.o_mu_v = C.mu_v; a.o_u_t = C.u_t;
-  a.o_mu_k16 = C.mu_k16; a.o_mu_v16 = C.mu_v16; a.o_e16 = C.e16;
-  a.cache = static_cast<const uint8_t*>(cache);
-  a.L = qwm::cache_layout(*cfg);
-  a.q = q; a.out = out; a.lse = lse_out; a.logits = logits_out;
-  a.n_cache = n_cache; a.n_q = n_q; a.q_start = q_start;
-  a.n_epochs = n_epochs;
-  a.calib_stride = n_epochs > 1 ? int64_t(quantwm_calib_bytes(cfg)) : 0;
-  for (int e = 0; e < qwm::kMaxEpochs; ++e) a.epoch_start[e] = e < n_epochs && n_epochs > 1 ? epoch_start[e] : 0;
-  a.k_act = n_act > 0 ? k_act : nullptr;
-  a.v_act = n_act > 0 ? v_act : nullptr;
-  a.n_act = n_act;
-  a.frame_tokens = frame_tokens; a.heads = cfg->heads; a.n_centroids = cfg->n_centroids; a.rank = cfg->rank;
-  a.tables_in_lds = tables ? 1 : 0;
-  a.n_split = 1;
-  a.part_o = nullptr;
-  a.part_ml = nullptr;
+  qwm::AttendArgs a = attend_args(cfg, calib, n_epochs, epoch_start, cache, n_cache, k_act, v_act, n_act, q, n_q,
+                                  q_start, frame_tokens, out, lse_out, logits_out);
+  if (window) {
+    a.windowed = 1;
+    a.n_sink = window->n_sink < n_cache + n_act ? window->n_sink : n_cache + n_act;
+    a.window = window->window;
+  }
   if (!logits_out && workspace) {
     if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(QWM_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     // the cheapest number of parts that the workspace holds
     int most = 1;
     while (most < qwm::kMaxSplits && planes_bytes(cfg, most + 1, n_q) <= workspace_bytes) ++most;
-    const int ns = qwm::attend_splits(n_q, cfg->heads, cfg->batch, n_cache + n_act, device_cus(), elem, most);
-    if (ns > 1) {
-      const size_t rows = size_t(ns) * cfg->batch * cfg->heads * size_t(n_q);
-      a.n_split = ns;
-      a.part_o = static_cast<float*>(workspace);
-      a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + (rows * cfg->head_dim * 4 + 255) / 256 * 256);
-    }
+    const int ns = qwm::attend_splits(n_q, cfg->heads, cfg->batch, keys_in_reach(n_cache + n_act, frame_tokens, window),
+                                      device_cus(), qwm::elem_bytes(*cfg), most);
+    if (ns > 1) set_planes(cfg, a, ns, workspace);
   }
   a.q_row0 = logits_out ? q_first : 0;
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -545,9 +592,7 @@ static quantwm_status attend_common(const quantwm_config* cfg, const void* calib
   // the kernel keeps Query and key positions in 32 bits
   if (n_q > kMaxPositions || n_cache + n_act > kMaxPositions)
     return fail(QWM_ERR_UNSUPPORTED, "more than %lld Queries or keys per head", (long long)kMaxPositions);
-  const bool lg = logits_out != nullptr;
-  const hipError_t e = cfg->dtype == QWM_BF16 ? qwm::launch_attend_bf16(a, cfg->head_dim, cfg->batch, lg, s)
-                                              : qwm::launch_attend_f32(a, cfg->head_dim, cfg->batch, lg, s);
+  const hipError_t e = launch_attend(cfg, a, logits_out != nullptr, s);
   if (e != hipSuccess) return hip_fail(e, "attend launch");
   return ok();
 }
@@ -574,6 +619,224 @@ quantwm_status quantwm_attend_epochs(const quantwm_config* cfg, const void* cali
                                      void* workspace, size_t workspace_bytes, void* stream) {
   return attend_common(cfg, calibs, n_epochs, epoch_start, cache, n_cache, k_act, v_act, n_act, q, n_q, q_start,
                        frame_tokens, out, lse_out, nullptr, workspace, workspace_bytes, stream);
+}
+
+static quantwm_status check_window(int64_t n_sink, int64_t window) {
+  if (n_sink < 0 || window < 0) return fail(QWM_ERR_INVALID_ARG, "n_sink and window must be >= 0");
+  return QWM_OK;
+}
+// bounds past any position, so that the kernel's sums with them stay in 64 bits
+static Window window_of(int64_t n_sink, int64_t window) {
+  const int64_t most = int64_t(1) << 40;
+  return {n_sink < most ? n_sink : most, window < most ? window : most};
+}
+
+size_t quantwm_attend_window_workspace_bytes(const quantwm_config* cfg, int64_t n_cache, int64_t n_act, int64_t n_q,
+                                             int32_t frame_tokens, int64_t n_sink, int64_t window) {
+  if (check_cfg(cfg) != QWM_OK || n_cache < 0 || n_act < 0 || n_q <= 0 || frame_tokens < 1) return 0;
+  if (check_window(n_sink, window) != QWM_OK) return 0;
+  const Window w = window_of(n_sink, window);
+  return attend_split_bytes(cfg, keys_in_reach(n_cache + n_act, frame_tokens, &w), n_q, nullptr);
+}
+
+quantwm_status quantwm_attend_window(const quantwm_config* cfg, const void* calibs, int32_t n_epochs,
+                                     const int64_t* epoch_start, const void* cache, int64_t n_cache,
+                                     const void* k_act, const void* v_act, int64_t n_act, const void* q, int64_t n_q,
+                                     int64_t q_start, int32_t frame_tokens, int64_t n_sink, int64_t window, void* out,
+                                     float* lse_out, void* workspace, size_t workspace_bytes, void* stream) {
+  QWM_TRY(check_window(n_sink, window));
+  const Window w = window_of(n_sink, window);
+  return attend_common(cfg, calibs, n_epochs, epoch_start, cache, n_cache, k_act, v_act, n_act, q, n_q, q_start,
+                       frame_tokens, out, lse_out, nullptr, workspace, workspace_bytes, stream, 0, &w);
+}
+
+// Key splits of the two passes of quantwm_attend_shared (0: no keys, no pass) and
+// the bytes of each one's partial planes.
+struct SharedPlan {
+  int prefix, own;
+  size_t prefix_bytes, own_bytes;
+};
+static SharedPlan shared_plan(const quantwm_config* prefix_cfg, int64_t n_prefix, const quantwm_config* cfg,
+                              int64_t n_own, int64_t n_q) {
+  SharedPlan p{0, 0, 0, 0};
+  const int cus = device_cus(), elem = qwm::elem_bytes(*cfg);
+  if (n_prefix > 0) {
+    p.prefix = qwm::attend_splits(n_q * cfg->batch, cfg->heads, 1, n_prefix, cus, elem);
+    p.prefix_bytes = size_t(qwm::align256(int64_t(planes_bytes(prefix_cfg, p.prefix, n_q * cfg->batch))));
+  }
+  if (n_own > 0) {
+    p.own = qwm::attend_splits(n_q, cfg->heads, cfg->batch, n_own, cus, elem);
+    p.own_bytes = planes_bytes(cfg, p.own, n_q);
+  }
+  return p;
+}
+
+static quantwm_status check_shared(const quantwm_config* prefix_cfg, int64_t n_prefix, const quantwm_config* cfg,
+                                   int64_t n_cache, int64_t n_act, int64_t n_q) {
+  QWM_TRY(check_cfg(prefix_cfg));
+  QWM_TRY(check_cfg(cfg));
+  if (prefix_cfg->batch != 1) return fail(QWM_ERR_INVALID_ARG, "the shared prefix's config must have batch 1");
+  if (prefix_cfg->heads != cfg->heads || prefix_cfg->head_dim != cfg->head_dim || prefix_cfg->dtype != cfg->dtype)
+    return fail(QWM_ERR_INVALID_ARG, "the two configs must agree in heads, head_dim and dtype");
+  if (n_prefix < 0 || n_cache < 0 || n_act < 0 || n_q < 0) return fail(QWM_ERR_INVALID_ARG, "sizes must be >= 0");
+  // Queries and keys are counted in 32 bits, the rollouts' rows together in the prefix pass
+  if (n_q > kMaxPositions / cfg->batch || n_prefix > kMaxPositions || n_cache + n_act > kMaxPositions)
+    return fail(QWM_ERR_UNSUPPORTED, "more than %lld Queries or keys per head", (long long)kMaxPositions);
+  return QWM_OK;
+}
+
+size_t quantwm_attend_shared_workspace_bytes(const quantwm_config* prefix_cfg, int64_t n_prefix,
+                                             const quantwm_config* cfg, int64_t n_cache, int64_t n_act, int64_t n_q) {
+  if (check_shared(prefix_cfg, n_prefix, cfg, n_cache, n_act, n_q) != QWM_OK || n_q == 0) return 0;
+  const SharedPlan p = shared_plan(prefix_cfg, n_prefix, cfg, n_cache + n_act, n_q);
+  return p.prefix_bytes + p.own_bytes;
+}
+
+quantwm_status quantwm_attend_shared(const quantwm_config* prefix_cfg, const void* prefix_calibs, int32_t n_epochs,
+                                     const int64_t* epoch_start, const void* prefix_cache, int64_t n_prefix,
+                                     const quantwm_config* cfg, const void* calib, const void* cache, int64_t n_cache,
+                                     const void* k_act, const void* v_act, int64_t n_act, const void* q, int64_t n_q,
+                                     int64_t q_start, int32_t frame_tokens, void* out, float* lse_out,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+  QWM_TRY(check_shared(prefix_cfg, n_prefix, cfg, n_cache, n_act, n_q));
+  if (q_start < n_prefix) return fail(QWM_ERR_INVALID_ARG, "q_start must be >= n_prefix: every Query sees the whole prefix");
+  // the rollouts' rows as one chunk behind the prefix, and each rollout's own keys
+  QWM_TRY(check_attend_sizes(prefix_cfg, n_epochs, epoch_start, n_prefix, 0, n_q * cfg->batch, n_prefix, 1));
+  QWM_TRY(check_attend_sizes(cfg, 1, nullptr, n_cache, n_act, n_q, q_start - n_prefix, frame_tokens));
+  if (n_q == 0) return ok();
+  const int64_t n_own = n_cache + n_act;
+  if (n_prefix > 0) {
+    QWM_TRY(check_dev(prefix_calibs, "prefix_calibs"));
+    QWM_TRY(check_dev(prefix_cache, "prefix_cache"));
+  }
+  if (n_own > 0) {
+    QWM_TRY(check_dev(calib, "calib"));
+    QWM_TRY(check_dev(cache, "cache"));
+  }
+  if (n_act > 0) {
+    QWM_TRY(check_dev(k_act, "k_act"));
+    QWM_TRY(check_dev(v_act, "v_act"));
+  }
+  QWM_TRY(check_dev(q, "q"));
+  QWM_TRY(check_dev(out, "out"));
+  if (lse_out && (reinterpret_cast<uintptr_t>(lse_out) & 3)) return fail(QWM_ERR_INVALID_ARG, "lse_out misaligned");
+  const SharedPlan p = shared_plan(prefix_cfg, n_prefix, cfg, n_own, n_q);
+  const size_t need = p.prefix_bytes + p.own_bytes;
+  if (need > 0) {
+    QWM_TRY(check_dev(workspace, "workspace"));
+    if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(QWM_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    if (workspace_bytes < need)
+      return fail(QWM_ERR_INVALID_ARG, "workspace too small: %zu < %zu bytes", workspace_bytes, need);
+  }
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  qwm::SharedArgs c{};
+  c.n_q = n_q; c.heads = cfg->heads; c.batch = cfg->batch; c.out = out; c.lse = lse_out;
+  if (p.prefix > 0) {
+    qwm::AttendArgs a = attend_args(prefix_cfg, prefix_calibs, n_epochs, epoch_start, prefix_cache, n_prefix, nullptr,
+                                    nullptr, 0, q, n_q * cfg->batch, n_prefix, 1, nullptr, nullptr, nullptr);
+    set_planes(prefix_cfg, a, p.prefix, workspace);
+    if ((e = launch_attend(prefix_cfg, a, false, s)) != hipSuccess) return hip_fail(e, "attend launch (prefix)");
+    c.prefix_o = a.part_o; c.prefix_ml = a.part_ml; c.n_prefix = p.prefix;
+  }
+  if (p.own > 0) {
+    qwm::AttendArgs a = attend_args(cfg, calib, 1, nullptr, cache, n_cache, k_act, v_act, n_act, q, n_q,
+                                    q_start - n_prefix, frame_tokens, nullptr, nullptr, nullptr);
+    set_planes(cfg, a, p.own, static_cast<uint8_t*>(workspace) + p.prefix_bytes);
+    if ((e = launch_attend(cfg, a, false, s)) != hipSuccess) return hip_fail(e, "attend launch (own keys)");
+    c.own_o = a.part_o; c.own_ml = a.part_ml; c.n_own = p.own;
+  }
+  if ((e = qwm::launch_shared_combine(c, cfg->head_dim, cfg->dtype == QWM_BF16, s)) != hipSuccess)
+    return hip_fail(e, "shared combine launch");
+  return ok();
+}
+
+quantwm_status quantwm_rotary_init(const quantwm_config* cfg, const int32_t* dims, int32_t height, int32_t width,
+                                   double base, int32_t pairs, quantwm_rotary_axes* out) {
+  QWM_TRY(check_cfg(cfg));
+  if (!dims || !out) return fail(QWM_ERR_INVALID_ARG, "dims or out is null");
+  if (!(base > 0.0) || !std::isfinite(base)) return fail(QWM_ERR_INVALID_ARG, "base must be finite and > 0");
+  quantwm_rotary_axes a{};
+  a.pairs = pairs;
+  a.height = height;
+  a.width = width;
+  int64_t sum = 0;
+  for (int i = 0; i < 3; ++i) {
+    a.dims[i] = dims[i];
+    if (dims[i] < 0 || dims[i] % 2) return fail(QWM_ERR_INVALID_ARG, "dims must be even and >= 0");
+    sum += dims[i];
+  }
+  if (sum > cfg->head_dim) return fail(QWM_ERR_INVALID_ARG, "dims sum to more than head_dim");
+  int p = 0;
+  for (int i = 0; i < 3; ++i)
+    for (int j = 0; j < dims[i] / 2; ++j) a.freq[p++] = std::pow(base, -2.0 * j / dims[i]);
+  *out = a;
+  return ok();
+}
+
+quantwm_status quantwm_rotary(const quantwm_config* cfg, const quantwm_rotary_axes* axes, int64_t pos0,
+                              const int32_t* pos, const void* q, const void* k, int64_t n, int64_t token_stride,
+                              void* q_out, void* k_out, int32_t inverse, void* stream) {
+  QWM_TRY(check_cfg(cfg));
+  if (!axes) return fail(QWM_ERR_INVALID_ARG, "axes is null");
+  const int64_t row = int64_t(cfg->heads) * cfg->head_dim;
+  if (n < 0) return fail(QWM_ERR_INVALID_ARG, "n must be >= 0");
+  if (axes->pairs != QWM_ROTARY_ADJACENT && axes->pairs != QWM_ROTARY_HALVES)
+    return fail(QWM_ERR_INVALID_ARG, "pairs must be QWM_ROTARY_ADJACENT or QWM_ROTARY_HALVES");
+  int64_t sum = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (axes->dims[i] < 0 || axes->dims[i] % 2) return fail(QWM_ERR_INVALID_ARG, "dims must be even and >= 0");
+    sum += axes->dims[i];
+  }
+  if (sum > cfg->head_dim) return fail(QWM_ERR_INVALID_ARG, "dims sum to more than head_dim");
+  if (axes->pairs == QWM_ROTARY_HALVES && sum % 16)
+    return fail(QWM_ERR_UNSUPPORTED, "with QWM_ROTARY_HALVES dims must sum to a multiple of 16");
+  for (int p = 0; p < sum / 2; ++p)
+    if (!std::isfinite(axes->freq[p])) return fail(QWM_ERR_INVALID_ARG, "freq[%d] is not finite", p);
+  if (n == 0) return ok();
+  QWM_TRY(check_dev(q, "q"));
+  QWM_TRY(check_dev(q_out, "q_out"));
+  if (!k != !k_out) return fail(QWM_ERR_INVALID_ARG, "k and k_out go together");
+  QWM_TRY(check_dev(k, "k", false));
+  QWM_TRY(check_dev(k_out, "k_out", false));
+  const int elem = qwm::elem_bytes(*cfg);
+  if (token_stride < row || token_stride * elem % 16 || token_stride > (int64_t(1) << 40))
+    return fail(QWM_ERR_INVALID_ARG, "token_stride must be at least heads * head_dim and a multiple of 16 bytes");
+  if (n > kMaxPositions / cfg->batch) return fail(QWM_ERR_UNSUPPORTED, "more than %lld tokens", (long long)kMaxPositions);
+  if (pos) {
+    if (reinterpret_cast<uintptr_t>(pos) & 3) return fail(QWM_ERR_INVALID_ARG, "pos is not 4-byte aligned");
+  } else {
+    if (axes->height < 1 || axes->width < 1) return fail(QWM_ERR_INVALID_ARG, "height and width must be >= 1");
+    const int64_t area = int64_t(axes->height) * axes->width;
+    if (pos0 < 0 || pos0 > (int64_t(1) << 60) || (pos0 + n - 1) / area > INT32_MAX)
+      return fail(QWM_ERR_INVALID_ARG, "positions must lie in [0, 2^31) on every axis");
+  }
+  // an output may be its own contiguous input; other overlaps would be read back turned
+  const int64_t tokens = n * cfg->batch;
+  const size_t in_bytes = size_t((tokens - 1) * token_stride + row) * elem, out_bytes = size_t(tokens * row) * elem;
+  auto apart = [](const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return !a || !b || x + na <= y || y + nb <= x;
+  };
+  auto fine = [&](const void* in, const void* o) { return apart(in, in_bytes, o, out_bytes); };
+  const bool same_ok = token_stride == row;
+  if (!(fine(q, q_out) || (same_ok && q == q_out)) || !(fine(k, k_out) || (same_ok && k == k_out)) || !fine(q, k_out) ||
+      !fine(k, q_out) || !apart(q_out, out_bytes, k_out, out_bytes) ||
+      !apart(pos, size_t(tokens) * 12, q_out, out_bytes) || !apart(pos, size_t(tokens) * 12, k_out, out_bytes))
+    return fail(QWM_ERR_INVALID_ARG, "buffers overlap (only an output equal to its own contiguous input may)");
+  qwm::RotaryArgs a;
+  a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out; a.pos = pos;
+  a.pos0 = pos0; a.n = n; a.tokens = tokens; a.token_stride = token_stride;
+  a.heads = cfg->heads; a.pairs = int(sum / 2);
+  a.end_t = axes->dims[0] / 2; a.end_h = a.end_t + axes->dims[1] / 2;
+  a.height = axes->height; a.width = axes->width;
+  a.sign = inverse ? -1.0f : 1.0f;
+  const double two_pi = 6.283185307179586476925286766559;
+  for (int p = 0; p < 64; ++p) a.turns[p] = p < a.pairs ? axes->freq[p] / two_pi : 0.0;
+  const hipError_t e = qwm::launch_rotary(a, cfg->head_dim, cfg->dtype == QWM_BF16, axes->pairs == QWM_ROTARY_HALVES,
+                                          static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "rotary launch");
+  return ok();
 }
 
 quantwm_status quantwm_attend_noalloc(const quantwm_config* cfg, const void* calib, const void* cache,

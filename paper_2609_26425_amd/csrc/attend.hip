@@ -99,6 +99,9 @@ struct Segment {
   int64_t lo, hi, base, tiles;
   int epoch;
   bool act;
+  // windowed launches: after the first `cut` tiles, `skip` tiles that no Query of
+  // the workgroup sees are left out (tiles does not count them)
+  int64_t cut, skip;
 };
 
 // Row of the 32x32 accumulator held by accumulator slot i of a lane in half hf.
@@ -258,7 +261,12 @@ __device__ inline V pack_operand(const float* x) {
 // plain launch per epoch and a merge of their partial planes. 28,080 packed keys
 // with 8-bit scales + 4,680 exact ones: 3.44 ms, against 5.02 ms in two merged
 // parts. (A plain launch over as many packed keys takes 3.28 ms.)
-template <typename T, int D, int RP, bool LOGITS, bool TAB, bool GEN, bool SI8>
+//
+// WIN (a GEN launch): a Query sees the first n_sink keys and the last `window`
+// positions up to the end of its own frame. Of every segment a workgroup runs
+// the tiles that hold a sink or a key of its first Query's window; the tiles
+// between them cost nothing, neither bytes nor products.
+template <typename T, int D, int RP, bool LOGITS, bool TAB, bool GEN, bool SI8, bool WIN>
 __global__ __launch_bounds__(NT) void attend_kernel(const AttendArgs a) {
   typedef Mfma<T> MF;
   typedef typename MF::V V;
@@ -322,8 +330,15 @@ __global__ __launch_bounds__(NT) void attend_kernel(const AttendArgs a) {
   const int64_t qoff = LOGITS ? a.q_row0 : 0;
   int64_t kfull = qs + ((qa + qoff) / F + 1) * F;  // keys below are visible to every Query of the workgroup
   if (kfull > nc) kfull = nc;
+  // WIN: keys [0, ns) and [w, ...) are in a row's reach, w = wlo for the first
+  // Query of the workgroup and wfull for the last one
+  auto window_from = [&](int64_t row) __attribute__((always_inline)) {
+    const int64_t w = qs + (row / F + 1) * F - a.window;
+    return w < 0 ? int64_t(0) : (w < nc ? w : nc);
+  };
+  const int64_t ns = WIN ? a.n_sink : 0, wlo = WIN ? window_from(qa) : 0, wfull = WIN ? window_from(qb - 1) : 0;
   auto segment = [&](int i) {
-    Segment g{0, kend, 0, (kend + KT - 1) / KT, 0, false};
+    Segment g{0, kend, 0, (kend + KT - 1) / KT, 0, false, 0, 0};
     if constexpr (GEN) {
       g.act = i == a.n_epochs;
       g.epoch = g.act ? 0 : i;
@@ -333,7 +348,18 @@ __global__ __launch_bounds__(NT) void attend_kernel(const AttendArgs a) {
       g.base = g.act ? npk : g.lo / KT * KT;
       g.tiles = g.hi > g.lo ? (g.hi - g.base + KT - 1) / KT : 0;
     }
+    if constexpr (WIN) {
+      const int64_t sink = ns > g.lo ? (ns - g.base + KT - 1) / KT : 0;
+      g.cut = sink < g.tiles ? sink : g.tiles;
+      const int64_t from = wlo >= g.hi ? g.tiles : (wlo > g.base ? (wlo - g.base) / KT : 0);
+      g.skip = from > g.cut ? from - g.cut : 0;
+      g.tiles -= g.skip;
+    }
     return g;
+  };
+  // first key of tile t of segment g
+  auto key_of = [&](const Segment& g, int64_t t) __attribute__((always_inline)) {
+    return g.base + (WIN && t >= g.cut ? t + g.skip : t) * KT;
   };
   // tiles of all segments; with several epochs a lane of the wave counts for each
   // (kMaxEpochs is the wave's size): one load, where a loop over them, here and up to
@@ -678,12 +704,12 @@ __global__ __launch_bounds__(NT) void attend_kernel(const AttendArgs a) {
     }
   };
 
-  // rows of the active chunk: keys 64 t .. 64 t + 63 of it; past its end the last
+  // rows of the active chunk: its keys r0 .. r0 + 63; past its end the last
   // row again (the mask hides those keys). The row is clamped, not guarded: with
   // a guard the compiler folded the per-lane condition into the tile loop (in its
   // assembly the loop then ends on the execution mask), and results were wrong.
-  auto load_act = [&](ActRegs<KW, VW>& p, int64_t t) __attribute__((always_inline)) {
-    const int64_t r0 = t * KT, last = a.n_act - 1;
+  auto load_act = [&](ActRegs<KW, VW>& p, int64_t r0) __attribute__((always_inline)) {
+    const int64_t last = a.n_act - 1;
     load_words(act_row(k_act, r0 + kkey < last ? r0 + kkey : last, kch0), p.k, KW);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
@@ -756,7 +782,7 @@ __global__ __launch_bounds__(NT) void attend_kernel(const AttendArgs a) {
   };
   float m_run = -__builtin_inff(), l_run = 0.0f;
   f32x16 oacc[D / 32];
-  int lim = int(nc);
+  int lim = int(nc), wfrom = 0;
   // O is held times 2^-ev, the binary16 Value table's scale. Between segments O moves
   // from one scale to the next; in the streaming forms ev stays within +-kMaxShift, so
   // that this neither overflows nor loses bits, and the rest of a table's exponent
@@ -815,6 +841,7 @@ __global__ __launch_bounds__(NT) void attend_kernel(const AttendArgs a) {
     if (qvalid) {
       const int64_t l = qs + ((qi + qoff) / F + 1) * F;  // this lane's Query sees keys j < lim
       lim = int(l < nc ? l : nc);
+      if constexpr (WIN) wfrom = int(window_from(qi));
     }
   }
   const float mscale = 1.4426950408889634f / sqrtf((float)D);  // logits are exponentiated as 2^(S log2(e)/sqrt(d))
@@ -830,14 +857,15 @@ __global__ __launch_bounds__(NT) void attend_kernel(const AttendArgs a) {
       if (GEN && g.act) {
         // exact keys: copied a tile ahead, in registers for one tile
         ActRegs<KW, VW> A;
-        load_act(A, ta);
+        auto load = [&](int64_t t) __attribute__((always_inline)) { load_act(A, key_of(g, t) - npk); };
+        load(ta);
         store_act(A, int(ta + par) & 1);
-        if (ta + 1 < te) load_act(A, ta + 1);
+        if (ta + 1 < te) load(ta + 1);
         for (int64_t it = ta; it < te; ++it) {
           __syncthreads();
           if (it + 1 < te) {
             store_act(A, int(it + 1 + par) & 1);
-            if (it + 2 < te) load_act(A, it + 2);
+            if (it + 2 < te) load(it + 2);
           }
         }
         return;
@@ -848,7 +876,7 @@ __global__ __launch_bounds__(NT) void attend_kernel(const AttendArgs a) {
       };
       const auto r_v = scales(g);
       auto prefetch = [&](TileRegs<NSUB>& p, int64_t t) __attribute__((always_inline)) {
-        load_raw(p, uint32_t(g.base + t * KT), AnyRows{}, r_v, int(g.lo));
+        load_raw(p, uint32_t(key_of(g, t)), AnyRows{}, r_v, int(g.lo));
       };
       int ek, en;
       table_exps(g.epoch, ek, en);
@@ -896,10 +924,10 @@ __global__ __launch_bounds__(NT) void attend_kernel(const AttendArgs a) {
         for (; it + 1 < nsteady; it += 2) {
           __syncthreads();
           dequant(P1, it + 1);
-          load_raw(P1, uint32_t(g.base + (it + 3) * KT), rows_tag, r_v, 0);
+          load_raw(P1, uint32_t(key_of(g, it + 3)), rows_tag, r_v, 0);
           __syncthreads();
           dequant(P0, it + 2);
-          load_raw(P0, uint32_t(g.base + (it + 4) * KT), rows_tag, r_v, 0);
+          load_raw(P0, uint32_t(key_of(g, it + 4)), rows_tag, r_v, 0);
         }
       };
       if (GEN && RP > 0 && L.sparse) steady(SparseRows{});
@@ -929,7 +957,7 @@ __global__ __launch_bounds__(NT) void attend_kernel(const AttendArgs a) {
   // it: tile of segment g, in buffer `buf`
   auto tile = [&](const Segment& g, int64_t it, int buf, auto mask_tag) {
     constexpr bool MASKED = decltype(mask_tag)::value;
-    const int64_t k0 = g.base + it * KT;
+    const int64_t k0 = key_of(g, it);
     __syncthreads();
     if (idle) return;
     const T* kt = smem + tile0 + buf * LY::tile_elems;
@@ -992,7 +1020,7 @@ __global__ __launch_bounds__(NT) void attend_kernel(const AttendArgs a) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int key = int(k0) + kb * 32 + acc_row(i, hf);
-            if (key >= khi || (GEN && key < klo)) sv[i] = -__builtin_inff();
+            if (key >= khi || (GEN && key < klo) || (WIN && key >= int(ns) && key < wfrom)) sv[i] = -__builtin_inff();
           }
         }
       };
@@ -1078,6 +1106,20 @@ __global__ __launch_bounds__(NT) void attend_kernel(const AttendArgs a) {
       __syncthreads();
     }
     const int64_t top = kfull < g.hi ? kfull : g.hi;
+    if constexpr (WIN) {
+      // runs of tiles with and without a mask in turn (a mask at the segment's and
+      // the sinks' ends, where the window opens and where the frame closes)
+      auto clean = [&](int64_t it) {
+        const int64_t k0 = key_of(g, it);
+        return k0 >= g.lo && k0 + KT <= top && (k0 + KT <= ns || k0 >= wfull);
+      };
+      int64_t it = ta;
+      while (it < te) {
+        for (; it < te && !clean(it); ++it) tile(g, it, int(it + par) & 1, std::integral_constant<bool, true>{});
+        for (; it < te && clean(it); ++it) tile(g, it, int(it + par) & 1, std::integral_constant<bool, false>{});
+      }
+      return;
+    }
     const int64_t nclean = (top - g.base) / KT < te ? (top - g.base) / KT : te;
     int64_t it = ta;
     if (GEN && it == 0 && g.lo > g.base) {  // the first tile holds keys of the segment before
@@ -1091,7 +1133,7 @@ __global__ __launch_bounds__(NT) void attend_kernel(const AttendArgs a) {
   if constexpr (!LOGITS) {
     if constexpr (GEN && H16) l_run = ldexpf(l_run, -psh);
     const float l_tot = l_run + __shfl_xor(l_run, 32);
-    if (a.n_split > 1) {
+    if (a.part_o) {
       // partial result of this split: unnormalised O, the running max (raw logit
       // units) and the sum; attend_combine merges the splits
       if (qvalid) {
@@ -1122,7 +1164,7 @@ __global__ __launch_bounds__(NT) void attend_kernel(const AttendArgs a) {
   }
 }
 
-template <typename T, int D, int RP, bool LOGITS, bool TAB, bool GEN = false, bool SI8 = false>
+template <typename T, int D, int RP, bool LOGITS, bool TAB, bool GEN = false, bool SI8 = false, bool WIN = false>
 hipError_t launch_k(const AttendArgs& a, const dim3& grid, size_t lds, hipStream_t s) {
   // the dynamic LDS limit is raised once per device for this instance
   static std::atomic<uint64_t> raised{0};
@@ -1131,12 +1173,12 @@ hipError_t launch_k(const AttendArgs& a, const dim3& grid, size_t lds, hipStream
   if (e != hipSuccess) return e;
   const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
   if (!bit || !(raised.load(std::memory_order_acquire) & bit)) {
-    e = hipFuncSetAttribute((const void*)attend_kernel<T, D, RP, LOGITS, TAB, GEN, SI8>,
+    e = hipFuncSetAttribute((const void*)attend_kernel<T, D, RP, LOGITS, TAB, GEN, SI8, WIN>,
                             hipFuncAttributeMaxDynamicSharedMemorySize, int(kLdsLimit));
     if (e != hipSuccess) return e;
     raised.fetch_or(bit, std::memory_order_release);
   }
-  hipLaunchKernelGGL((attend_kernel<T, D, RP, LOGITS, TAB, GEN, SI8>), grid, dim3(NT), lds, s, a);
+  hipLaunchKernelGGL((attend_kernel<T, D, RP, LOGITS, TAB, GEN, SI8, WIN>), grid, dim3(NT), lds, s, a);
   return hipGetLastError();
 }
 
@@ -1154,6 +1196,13 @@ hipError_t launch_attend_rp(const AttendArgs& a, int batch, bool logits, hipStre
       return tab ? launch_k<T, D, RP, true, true, false, true>(a, grid, lds, s)
                  : launch_k<T, D, RP, true, false, false, true>(a, grid, lds, s);
     return tab ? launch_k<T, D, RP, true, true>(a, grid, lds, s) : launch_k<T, D, RP, true, false>(a, grid, lds, s);
+  }
+  if (a.windowed) {
+    if (si8)
+      return tab ? launch_k<T, D, RP, false, true, true, true, true>(a, grid, lds, s)
+                 : launch_k<T, D, RP, false, false, true, true, true>(a, grid, lds, s);
+    return tab ? launch_k<T, D, RP, false, true, true, false, true>(a, grid, lds, s)
+               : launch_k<T, D, RP, false, false, true, false, true>(a, grid, lds, s);
   }
   // the general instance: an active chunk, calibration epochs, or sparse PSAC rows
   if (a.n_act > 0 || a.n_epochs > 1 || a.L.sparse) {

@@ -57,19 +57,74 @@ __global__ __launch_bounds__(256) void attend_combine(const AttendArgs a) {
   if (a.lse && lane == 0) a.lse[bh * a.n_q + qi] = L > 0.0f ? M / sqrtf((float)D) + logf(L) : -__builtin_inff();
 }
 
+// attend_combine over two sets of planes: those of the shared prefix, whose rows
+// are the rollouts' rows one after the other, and those of the own keys. One wave
+// per output row, in the order of the output.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void shared_combine(const SharedArgs a) {
+  const int64_t row = int64_t(blockIdx.x) * 4 + threadIdx.x / 64, rows = int64_t(a.batch) * a.n_q * a.heads;
+  const int lane = threadIdx.x % 64;
+  if (row >= rows) return;
+  const int64_t bi = row / a.heads, b = bi / a.n_q, i = bi % a.n_q;  // bi: row of the prefix pass
+  const int h = int(row % a.heads);
+  const int64_t at1 = h * (a.batch * a.n_q) + bi, at2 = (b * a.heads + h) * a.n_q + i;
+  const float mscale = 1.4426950408889634f / sqrtf((float)D);
+  constexpr int PL = D / 64;
+  typedef float vecf __attribute__((ext_vector_type(PL)));
+  const float2* ml1 = reinterpret_cast<const float2*>(a.prefix_ml) + at1;
+  const float2* ml2 = reinterpret_cast<const float2*>(a.own_ml) + at2;
+  const float* o1 = a.prefix_o + at1 * D + lane * PL;
+  const float* o2 = a.own_o + at2 * D + lane * PL;
+  float M = -__builtin_inff();
+  for (int sp = 0; sp < a.n_prefix; ++sp) M = fmaxf(M, ml1[sp * rows].x);
+  for (int sp = 0; sp < a.n_own; ++sp) M = fmaxf(M, ml2[sp * rows].x);
+  vecf o = {};
+  float L = 0.0f;
+  auto add = [&](const float2 p, const vecf v) __attribute__((always_inline)) {
+    if (!(p.y > 0.0f)) return;  // no visible key of this row in that part
+    const float w = __builtin_amdgcn_exp2f((p.x - M) * mscale);
+    L += w * p.y;
+#pragma unroll
+    for (int j = 0; j < PL; ++j) o[j] += w * v[j];
+  };
+#pragma unroll 4
+  for (int sp = 0; sp < a.n_prefix; ++sp) add(ml1[sp * rows], *reinterpret_cast<const vecf*>(o1 + sp * rows * D));
+#pragma unroll 4
+  for (int sp = 0; sp < a.n_own; ++sp) add(ml2[sp * rows], *reinterpret_cast<const vecf*>(o2 + sp * rows * D));
+  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  T* orow = reinterpret_cast<T*>(a.out) + row * D + lane * PL;
+#pragma unroll
+  for (int j = 0; j < PL; ++j) orow[j] = T(o[j] * inv);
+  if (a.lse && lane == 0) a.lse[at2] = L > 0.0f ? M / sqrtf((float)D) + logf(L) : -__builtin_inff();
+}
+
+template <typename T>
+hipError_t launch_shared_combine_t(const SharedArgs& a, int d, hipStream_t s) {
+  const int64_t rows = int64_t(a.batch) * a.n_q * a.heads;
+  const dim3 grid((unsigned)((rows + 3) / 4));
+  if (d == 64) hipLaunchKernelGGL((shared_combine<T, 64>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((shared_combine<T, 128>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
 template <typename T, int D>
 hipError_t launch_d(const AttendArgs& a, int batch, bool logits, hipStream_t s) {
   hipError_t e;
   if (a.rank == 0) e = launch_attend_rp<T, D, 0>(a, batch, logits, s);
   else if (a.rank <= 16) e = launch_attend_rp<T, D, 16>(a, batch, logits, s);
   else e = launch_attend_rp<T, D, 32>(a, batch, logits, s);
-  if (e != hipSuccess || logits || a.n_split == 1) return e;
+  // planes without an output: the caller joins them with others
+  if (e != hipSuccess || logits || a.n_split == 1 || !a.out) return e;
   hipLaunchKernelGGL((attend_combine<T, D>), dim3((unsigned)((a.n_q + 3) / 4), (unsigned)a.heads, (unsigned)batch),
                      dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
+
+hipError_t launch_shared_combine(const SharedArgs& a, int d, bool bf16_out, hipStream_t s) {
+  return bf16_out ? launch_shared_combine_t<bf16>(a, d, s) : launch_shared_combine_t<float>(a, d, s);
+}
 
 size_t attend_lds_bytes(int d, int elem, int rank, int n_centroids, bool tables) {
   if (elem == 2) return d == 64 ? attend_lds_bytes_t<bf16, 64>(rank, n_centroids, tables)

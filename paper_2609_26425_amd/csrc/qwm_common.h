@@ -142,9 +142,38 @@ struct AttendArgs {
   int n_epochs;
   int64_t calib_stride;
   int64_t epoch_start[64];
-  float* part_o;  // [n_split][B*H][n_q][d] unnormalised partial outputs (n_split > 1)
+  float* part_o;  // [n_split][B*H][n_q][d] unnormalised partial outputs; NULL: out and lse are written
   float* part_ml; // [n_split][B*H][n_q][2] running max (raw logits) and sum per partial
   int64_t q_row0;  // logits hook only: chunk row of the first Query (frame count of the mask)
+  // windowed: of the keys that the frame mask shows, a Query sees the first n_sink
+  // (at most the key count) and those of the last `window` positions up to the end of
+  // its frame
+  int windowed;
+  int64_t n_sink, window;
+};
+
+// Joins the partial planes of attention over a shared prefix (one chunk of all
+// rollouts' rows: [n_prefix][H][batch * n_q]) with those over each rollout's own
+// keys ([n_own][batch * H][n_q]).
+struct SharedArgs {
+  const float *prefix_o, *prefix_ml, *own_o, *own_ml;
+  int n_prefix, n_own;  // planes of each, 0 where there are no such keys
+  int64_t n_q;
+  int heads, batch;
+  void* out;
+  float* lse;
+};
+
+struct RotaryArgs {
+  const void *q, *k;  // [tokens][heads][d], rows token_stride elements apart; k may be NULL
+  void *q_out, *k_out;
+  const int32_t* pos;  // [tokens][3], or NULL: token i of a batch entry is pos0 + i of the frame grid
+  int64_t pos0, n, tokens, token_stride;
+  int heads, pairs;        // turned pairs of a head
+  int end_t, end_h;        // pairs [0, end_t) turn by time, [end_t, end_h) by height, the rest by width
+  int height, width;
+  float sign;              // -1: the inverse turn
+  double turns[64];        // turns (angle / 2 pi) per unit of position
 };
 
 // keys per attention tile
@@ -166,6 +195,8 @@ template <int D, int G>
 hipError_t launch_append_bf16(const AppendArgs& a, int batch, hipStream_t s);
 hipError_t launch_attend_f32(const AttendArgs& a, int d, int batch, bool logits, hipStream_t s);
 hipError_t launch_attend_bf16(const AttendArgs& a, int d, int batch, bool logits, hipStream_t s);
+hipError_t launch_shared_combine(const SharedArgs& a, int d, bool bf16_out, hipStream_t s);
+hipError_t launch_rotary(const RotaryArgs& a, int d, bool bf16_data, bool halves, hipStream_t s);
 size_t attend_lds_bytes(int d, int elem, int rank, int n_centroids, bool tables_in_lds);
 constexpr int kMaxSplits = 16;
 int attend_splits(int64_t n_q, int heads, int batch, int64_t n_cache, int cus, int elem, int most = kMaxSplits);

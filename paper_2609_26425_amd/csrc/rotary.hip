@@ -1,0 +1,156 @@
+// Rotary positions on three axes (time, height, width) for the Queries and Keys of
+// a chunk: pair p of a head's channels is turned by the angle a = x[axis(p)] f_p,
+//     (u, v) -> (u cos a - v sin a, u sin a + v cos a).
+// The angle depends on the token and the pair, not on the head: a workgroup takes
+// a few whole tokens, computes their cosines and sines once into LDS, and turns
+// every head of the Queries and the Keys with them. A far position's angle needs
+// more than fp32: turns = x f / 2 pi is formed and reduced to [-1/2, 1/2] in fp64,
+// and only the remainder goes to fp32 (2^-25 of a turn), so the cosines are right
+// to fp32 for any position. Memory bound: every value is read once and written
+// once.
+#include "qwm_common.h"
+
+namespace qwm {
+namespace {
+
+constexpr int kRotThreads = 256;
+
+template <typename T>
+struct Vec16 {  // 16 bytes of T as floats
+  static constexpr int N = 16 / int(sizeof(T));
+  float x[N];
+};
+
+template <typename T>
+__device__ inline Vec16<T> unpack(const uint4 u) {
+  Vec16<T> r;
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      r.x[2 * i] = __uint_as_float(w[i] << 16);
+      r.x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    } else {
+      r.x[i] = __uint_as_float(w[i]);
+    }
+  }
+  return r;
+}
+
+// The one rounding of the result (to nearest even in BF16).
+template <typename T>
+__device__ inline uint4 pack(const Vec16<T>& v) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+      typedef float f32x2 __attribute__((ext_vector_type(2)));
+      const f32x2 p = {v.x[2 * i], v.x[2 * i + 1]};
+      w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+    } else {
+      w[i] = __float_as_uint(v.x[i]);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// TT tokens per workgroup. HALVES: pair p is channels (p, p + pairs), so a thread
+// holds a vector of each half; otherwise it is channels (2 p, 2 p + 1) of one vector.
+// Channels past the turned pairs (p >= pairs) are copied, through cos 1 and sin 0.
+template <typename T, int D, bool HALVES, int TT>
+__global__ __launch_bounds__(kRotThreads) void rotary_kernel(const RotaryArgs a) {
+  constexpr int P = D / 2, N = Vec16<T>::N, UNIT = HALVES ? 2 * N : N, UNITS = D / UNIT;
+  __shared__ __attribute__((aligned(16))) float2 cs[TT * P];
+  const int64_t tok0 = int64_t(blockIdx.x) * TT;
+  const int tokens = int(a.tokens - tok0 < TT ? a.tokens - tok0 : TT);
+  for (int i = threadIdx.x; i < tokens * P; i += kRotThreads) {
+    const int p = i % P;
+    const int64_t tok = tok0 + i / P;
+    float2 v = make_float2(1.0f, 0.0f);
+    if (p < a.pairs) {
+      const int axis = p < a.end_t ? 0 : (p < a.end_h ? 1 : 2);
+      int64_t x;
+      if (a.pos) {
+        x = a.pos[tok * 3 + axis];
+      } else {
+        const int64_t at = a.pos0 + tok % a.n, area = int64_t(a.height) * a.width;
+        const int64_t in = at % area;
+        x = axis == 0 ? at / area : (axis == 1 ? in / a.width : in % a.width);
+      }
+      const double t = double(x) * a.turns[p];
+      const float rest = float(t - rint(t));
+      sincospif(2.0f * rest, &v.y, &v.x);
+      v.y *= a.sign;
+    }
+    cs[i] = v;
+  }
+  __syncthreads();
+
+  const int row = a.heads * UNITS, total = tokens * row;
+  const int64_t out_stride = int64_t(a.heads) * D;
+  auto turn = [&](const T* in, T* out, const float2* c, int first, int second) __attribute__((always_inline)) {
+    if constexpr (HALVES) {
+      Vec16<T> u = unpack<T>(*reinterpret_cast<const uint4*>(in + first));
+      Vec16<T> v = unpack<T>(*reinterpret_cast<const uint4*>(in + second));
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float2 t = c[j];
+        const float x = u.x[j], y = v.x[j];
+        u.x[j] = __builtin_fmaf(x, t.x, -y * t.y);
+        v.x[j] = __builtin_fmaf(x, t.y, y * t.x);
+      }
+      *reinterpret_cast<uint4*>(out + first) = pack<T>(u);
+      *reinterpret_cast<uint4*>(out + second) = pack<T>(v);
+    } else {
+      Vec16<T> u = unpack<T>(*reinterpret_cast<const uint4*>(in + first));
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) {
+        const float2 t = c[j];
+        const float x = u.x[2 * j], y = u.x[2 * j + 1];
+        u.x[2 * j] = __builtin_fmaf(x, t.x, -y * t.y);
+        u.x[2 * j + 1] = __builtin_fmaf(x, t.y, y * t.x);
+      }
+      *reinterpret_cast<uint4*>(out + first) = pack<T>(u);
+    }
+  };
+  for (int i = threadIdx.x; i < total; i += kRotThreads) {
+    const int t = i / row, u = i % row, h = u / UNITS, c = u % UNITS;
+    int first, second = 0, pair;
+    if constexpr (HALVES) {
+      const int turned = a.pairs / N;  // units of the turned channels
+      pair = c * N;
+      first = c < turned ? c * N : 2 * a.pairs + (c - turned) * 2 * N;
+      second = c < turned ? first + a.pairs : first + N;
+    } else {
+      pair = c * (N / 2);
+      first = c * N;
+    }
+    const int64_t src = (tok0 + t) * a.token_stride + h * D, dst = (tok0 + t) * out_stride + h * D;
+    turn(static_cast<const T*>(a.q) + src, static_cast<T*>(a.q_out) + dst, cs + t * P + pair, first, second);
+    if (a.k) turn(static_cast<const T*>(a.k) + src, static_cast<T*>(a.k_out) + dst, cs + t * P + pair, first, second);
+  }
+}
+
+template <typename T, int D, bool HALVES>
+hipError_t launch_t(const RotaryArgs& a, hipStream_t s) {
+  constexpr int TT = 4;
+  hipLaunchKernelGGL((rotary_kernel<T, D, HALVES, TT>), dim3((unsigned)((a.tokens + TT - 1) / TT)), dim3(kRotThreads), 0, s,
+                     a);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t launch_d(const RotaryArgs& a, bool halves, hipStream_t s) {
+  return halves ? launch_t<T, D, true>(a, s) : launch_t<T, D, false>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_rotary(const RotaryArgs& a, int d, bool bf16_data, bool halves, hipStream_t s) {
+  if (d == 64) return bf16_data ? launch_d<bf16, 64>(a, halves, s) : launch_d<float, 64>(a, halves, s);
+  if (d == 128) return bf16_data ? launch_d<bf16, 128>(a, halves, s) : launch_d<float, 128>(a, halves, s);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace qwm

@@ -46,6 +46,12 @@ class CalibLayout(ctypes.Structure):
                  "mu_k16", "mu_v16", "e16", "a_k3")]
 
 
+class RotaryAxes(ctypes.Structure):
+    """Mirror of quantwm_rotary_axes."""
+    _fields_ = [("pairs", ctypes.c_int32), ("dims", ctypes.c_int32 * 3), ("height", ctypes.c_int32),
+                ("width", ctypes.c_int32), ("freq", ctypes.c_double * 64)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with paper_2609_26425_amd/build.py "
@@ -74,6 +80,15 @@ def _load():
         "quantwm_attend_noalloc": (I32, [C, P, P, I64, P, I64, I64, I32, P, P, P]),
         "quantwm_attend_active_workspace_bytes": (SZ, [C, I64, I64, I64]),
         "quantwm_attend_epochs_workspace_bytes": (SZ, [C, I32, ctypes.POINTER(I64), I64, I64, I64]),
+        "quantwm_attend_window": (I32, [C, P, I32, ctypes.POINTER(I64), P, I64, P, P, I64, P, I64, I64, I32, I64, I64,
+                                        P, P, P, SZ, P]),
+        "quantwm_attend_window_workspace_bytes": (SZ, [C, I64, I64, I64, I32, I64, I64]),
+        "quantwm_attend_shared": (I32, [C, P, I32, ctypes.POINTER(I64), P, I64, C, P, P, I64, P, P, I64, P, I64, I64,
+                                        I32, P, P, P, SZ, P]),
+        "quantwm_attend_shared_workspace_bytes": (SZ, [C, I64, C, I64, I64, I64]),
+        "quantwm_rotary_init": (I32, [C, ctypes.POINTER(I32), I32, I32, ctypes.c_double, I32,
+                                      ctypes.POINTER(RotaryAxes)]),
+        "quantwm_rotary": (I32, [C, ctypes.POINTER(RotaryAxes), I64, P, P, P, I64, I64, P, P, I32, P]),
         "quantwm_coef_record_max_bytes": (SZ, [C, I64]),
         "quantwm_coef_pack": (I32, [C, P, I64, I64, P, SZ, ctypes.POINTER(I64), ctypes.POINTER(I32), P]),
         "quantwm_coef_unpack": (I32, [C, P, SZ, P, I64, I64, P]),
@@ -95,6 +110,8 @@ EXPORTED = ("quantwm_cache_bytes", "quantwm_token_bytes", "quantwm_calib_bytes",
             "quantwm_attend_epochs", "quantwm_attend_noalloc",
             "quantwm_logits", "quantwm_attend_active_workspace_bytes", "quantwm_attend_epochs_workspace_bytes", "quantwm_coef_record_max_bytes", "quantwm_coef_pack", "quantwm_coef_unpack",
             "quantwm_coef_pool_usage",
+            "quantwm_attend_window", "quantwm_attend_window_workspace_bytes", "quantwm_attend_shared",
+            "quantwm_attend_shared_workspace_bytes", "quantwm_rotary_init", "quantwm_rotary",
             "quantwm_last_error")
 
 
@@ -245,6 +262,132 @@ def quantwm_attend_epochs_workspace_bytes(cfg, epoch_start, n_cache, n_act, n_q)
     starts = (ctypes.c_int64 * len(epoch_start))(*[int(x) for x in epoch_start])
     return int(_lib.quantwm_attend_epochs_workspace_bytes(ctypes.byref(cfg), len(epoch_start), starts, n_cache,
                                                           n_act, n_q))
+
+
+def _check_tensors(dtype, **sized):
+    """Refuses, before a pointer is taken, tensors of another type, too small for
+    the call, or on another device than the one it runs on. sized: name -> (tensor
+    or None, least number of elements, dtype or None for the call's)."""
+    for name, (t, least, dt) in sized.items():
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name}: expected a torch.Tensor or None")
+        if t.dtype != (dt or dtype):
+            raise ValueError(f"{name}: expected {dt or dtype}, got {t.dtype}")
+        if t.numel() < least:
+            raise ValueError(f"{name}: {t.numel()} elements, the call needs {least}")
+        if torch.cuda.is_available() and (not t.is_cuda or t.device.index != torch.cuda.current_device()):
+            raise ValueError(f"{name}: on {t.device}, the call runs on cuda:{torch.cuda.current_device()}")
+
+
+def _ws_bytes(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def _attend_tensors(cfg, calib, blocks, cache, k_act, v_act, n_act, q, n_q, out, lse_out):
+    row = cfg.heads * cfg.head_dim
+    _check_tensors(cfg.torch_dtype, k_act=(k_act, cfg.batch * n_act * row, None),
+                   v_act=(v_act, cfg.batch * n_act * row, None), q=(q, cfg.batch * n_q * row, None),
+                   out=(out, cfg.batch * n_q * row, None), lse_out=(lse_out, cfg.batch * cfg.heads * n_q, torch.float32),
+                   calib=(calib, blocks * quantwm_calib_bytes(cfg), torch.uint8),
+                   cache=(cache, quantwm_cache_bytes(cfg), torch.uint8))
+
+
+def quantwm_attend_window(cfg, calibs, epoch_start, cache, n_cache, k_act, v_act, n_act, q, n_q, q_start,
+                          frame_tokens, n_sink, window, out, lse_out=None, workspace=None, stream=None):
+    """Attention over the first n_sink keys and the last `window` positions up to the
+    end of the Query's frame. calibs: one device buffer of len(epoch_start)
+    calibration blocks; epoch_start: host ints, [0] for a single block."""
+    starts = (ctypes.c_int64 * len(epoch_start))(*[int(x) for x in epoch_start])
+    _attend_tensors(cfg, calibs, len(epoch_start), cache, k_act, v_act, n_act, q, n_q, out, lse_out)
+    _check_tensors(torch.uint8, workspace=(workspace, 0, workspace.dtype if workspace is not None else None))
+    _check(_lib.quantwm_attend_window(ctypes.byref(cfg), _ptr(calibs), len(epoch_start), starts, _ptr(cache), n_cache,
+                                      _ptr(k_act), _ptr(v_act), n_act, _ptr(q), n_q, q_start, frame_tokens, n_sink,
+                                      window, _ptr(out), _ptr(lse_out), _ptr(workspace), _ws_bytes(workspace),
+                                      _stream(stream)))
+
+
+def quantwm_attend_window_workspace_bytes(cfg, n_cache, n_act, n_q, frame_tokens, n_sink, window) -> int:
+    return int(_lib.quantwm_attend_window_workspace_bytes(ctypes.byref(cfg), n_cache, n_act, n_q, frame_tokens, n_sink,
+                                                          window))
+
+
+def quantwm_attend_shared(prefix_cfg, prefix_calibs, epoch_start, prefix_cache, n_prefix, cfg, calib, cache, n_cache,
+                          k_act, v_act, n_act, q, n_q, q_start, frame_tokens, out, lse_out=None, workspace=None,
+                          stream=None):
+    """Attention of cfg.batch rollouts over [one shared prefix | own packed keys |
+    own exact keys]. prefix_calibs: len(epoch_start) calibration blocks of
+    prefix_cfg; workspace: quantwm_attend_shared_workspace_bytes() bytes."""
+    starts = (ctypes.c_int64 * len(epoch_start))(*[int(x) for x in epoch_start])
+    _attend_tensors(cfg, calib, 1, cache, k_act, v_act, n_act, q, n_q, out, lse_out)
+    _check_tensors(torch.uint8, workspace=(workspace, 0, workspace.dtype if workspace is not None else None),
+                   prefix_calibs=(prefix_calibs, len(epoch_start) * quantwm_calib_bytes(prefix_cfg), None),
+                   prefix_cache=(prefix_cache, quantwm_cache_bytes(prefix_cfg), None))
+    _check(_lib.quantwm_attend_shared(ctypes.byref(prefix_cfg), _ptr(prefix_calibs), len(epoch_start), starts,
+                                      _ptr(prefix_cache), n_prefix, ctypes.byref(cfg), _ptr(calib), _ptr(cache),
+                                      n_cache, _ptr(k_act), _ptr(v_act), n_act, _ptr(q), n_q, q_start, frame_tokens,
+                                      _ptr(out), _ptr(lse_out), _ptr(workspace), _ws_bytes(workspace),
+                                      _stream(stream)))
+
+
+def quantwm_attend_shared_workspace_bytes(prefix_cfg, n_prefix, cfg, n_cache, n_act, n_q) -> int:
+    return int(_lib.quantwm_attend_shared_workspace_bytes(ctypes.byref(prefix_cfg), n_prefix, ctypes.byref(cfg),
+                                                          n_cache, n_act, n_q))
+
+
+# Pairs of channels that rotary positions turn (QWM_ROTARY_* in include/quantwm.h)
+ROTARY_ADJACENT = 0
+ROTARY_HALVES = 1
+
+
+def rotary_axes(cfg, dims, height, width, base=10000.0, pairs=ROTARY_ADJACENT, freq=None) -> RotaryAxes:
+    """The axes of quantwm_rotary: dims = channels of time, height and width, a frame
+    of height x width tokens, freq = base^(-2 i / D) for pair i of an axis with D
+    channels (or the given radians per unit of position, one per pair)."""
+    out = RotaryAxes()
+    _check(_lib.quantwm_rotary_init(ctypes.byref(cfg), (ctypes.c_int32 * 3)(*dims), height, width, base, pairs,
+                                    ctypes.byref(out)))
+    if freq is not None:
+        if len(freq) != sum(dims) // 2:
+            raise ValueError(f"freq: {len(freq)} values for {sum(dims) // 2} pairs")
+        for p, f in enumerate(freq):
+            out.freq[p] = float(f)
+    return out
+
+
+def _token_rows(cfg, name, t, n):
+    """Elements from one token to the next of a [B, n, H, d] tensor whose tokens may
+    lie apart (a slice of a fused projection)."""
+    shape = (cfg.batch, n, cfg.heads, cfg.head_dim)
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    row = cfg.heads * cfg.head_dim
+    if n * cfg.batch <= 1:
+        step = row
+    else:
+        step = t.stride(1) if n > 1 else t.stride(0)
+    inner = (cfg.heads == 1 or t.stride(2) == cfg.head_dim) and t.stride(3) == 1
+    if not inner or (cfg.batch > 1 and t.stride(0) != n * step):
+        raise ValueError(f"{name}: heads and channels must be contiguous and the tokens evenly spaced")
+    return step
+
+
+def quantwm_rotary(cfg, axes, q, k, n, q_out, k_out=None, pos0=0, pos=None, inverse=False, stream=None):
+    """Turns q and k ([B, n, H, d]; k may be None) by their tokens' positions into
+    contiguous q_out and k_out: place pos0 + i of the frame grid, or pos ([B, n, 3]
+    int32). inverse: the transpose, which is the gradient."""
+    if n == 0:
+        return
+    row = cfg.heads * cfg.head_dim
+    _check_tensors(cfg.torch_dtype, q=(q, 0, None), k=(k, 0, None), q_out=(q_out, cfg.batch * n * row, None),
+                   k_out=(k_out, cfg.batch * n * row, None), pos=(pos, cfg.batch * n * 3, torch.int32))
+    step = _token_rows(cfg, "q", q, n)
+    if k is not None and _token_rows(cfg, "k", k, n) != step:
+        raise ValueError("q and k must have the same token stride")
+    _check(_lib.quantwm_rotary(ctypes.byref(cfg), ctypes.byref(axes), pos0, _ptr(pos),
+                               ctypes.c_void_p(q.data_ptr()), None if k is None else ctypes.c_void_p(k.data_ptr()), n,
+                               step, _ptr(q_out), _ptr(k_out), int(inverse), _stream(stream)))
 
 
 ATTEND_NOALLOC_SCRATCH_BYTES = 128 << 20  # QWM_ATTEND_NOALLOC_SCRATCH_BYTES

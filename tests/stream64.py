@@ -1,0 +1,119 @@
+"""Packed streams for the attention tests (quantised by the CPU oracle) and the plain
+64-bit softmax that the kernels are compared with: every logit from the oracle, with
+no mask, then masks and sums in numpy."""
+from __future__ import annotations
+
+import numpy as np
+import torch
+
+import oracle
+from paper_2609_26425_amd import quantwm as qw
+
+DEV = "cuda:0"
+
+
+def rounded(x, dtype):
+    t = torch.from_numpy(np.ascontiguousarray(x, np.float32))
+    return (t.bfloat16().float() if dtype == "bf16" else t).numpy()
+
+
+def dev(x, dt):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(DEV, dt)
+
+
+class Packed:
+    """n tokens per (b, h) appended in epochs at `starts`, each with its own tables."""
+
+    def __init__(self, rng, batch, heads, d, kc, g, r, dtype, storage, starts, n, capacity=None):
+        self.dtype, self.starts, self.n, self.r, self.d = dtype, list(starts), n, r, d
+        self.batch, self.heads = batch, heads
+        cap = max(1, n if capacity is None else capacity)
+        self.ocfg = oracle.cfg_of(batch, heads, d, kc, g, r, 4, cap, dtype == "bf16", storage)
+        self.cfg = qw.make_config(batch, heads, d, kc, g, r, 4, cap, dtype, storage)
+        self.cache, self.tables = oracle.new_cache(self.ocfg), []
+        for lo, hi in zip(self.starts, self.starts[1:] + [n]):
+            mu = [rounded(rng.standard_normal((batch, heads, kc, d)), dtype) for _ in range(2)]
+            u = np.stack([np.linalg.qr(rng.standard_normal((d, d)))[0][:r] for _ in range(batch * heads)])
+            t = (*mu, np.ones((batch, heads, d), np.float32), rounded(u.reshape(batch, heads, r, d), dtype),
+                 np.ones((batch, heads, r), np.float32))
+            if hi > lo:
+                k, v = (rounded(rng.standard_normal((batch, hi - lo, heads, d)), dtype) for _ in range(2))
+                oracle.append(self.ocfg, t, self.cache, lo, k, v)
+            self.tables.append(t)
+
+    def blocks(self):
+        """The calibration blocks on the device, one after the other."""
+        nb = qw.quantwm_calib_bytes(self.cfg)
+        out = torch.zeros(nb * len(self.tables), dtype=torch.uint8, device=DEV)
+        dt = self.cfg.torch_dtype
+        for e, t in enumerate(self.tables):
+            qw.quantwm_calib_pack(self.cfg, dev(t[0], dt), dev(t[1], dt), dev(t[2], torch.float32),
+                                  dev(t[3], dt) if self.r else None, dev(t[4], torch.float32) if self.r else None,
+                                  out[e * nb:(e + 1) * nb])
+        return out
+
+    def on_device(self):
+        return torch.from_numpy(self.cache).to(DEV)
+
+    def keys_values(self):
+        """Reconstructed Keys and Values as the attention's operands, [B, H, n, d]."""
+        k, v = np.zeros((2, self.batch, self.heads, self.n, self.d))
+        for lo, hi, t in zip(self.starts, self.starts[1:] + [self.n], self.tables):
+            if hi > lo:
+                for b in range(self.batch):
+                    for h in range(self.heads):
+                        dk, _, dv = oracle.decode(self.ocfg, t, self.cache, b, h, hi)
+                        k[b, h, lo:hi], v[b, h, lo:hi] = rounded(dk[lo:hi], self.dtype), rounded(dv[lo:hi], self.dtype)
+        return k, v
+
+    def logits(self, q):
+        """Every Query against every packed key, [B, H, n_q, n], in 64 bits."""
+        if self.n == 0:
+            return np.zeros((self.batch, self.heads, q.shape[1], 0))
+        _, _, lg = oracle.attend(self.ocfg, None, self.cache, self.n, q, self.n, 1, want_logits=True,
+                                 epochs=list(zip(self.starts, self.tables)))
+        return lg.reshape(self.batch, self.heads, q.shape[1], self.n)
+
+
+def exact_logits(q, k_act):
+    """[B, n_q, H, d] against [B, n_act, H, d] -> [B, H, n_q, n_act]."""
+    q, k = (np.ascontiguousarray(x.transpose(0, 2, 1, 3)).astype(np.float64) for x in (q, k_act))
+    return np.matmul(q, k.transpose(0, 1, 3, 2)) / np.sqrt(q.shape[-1])
+
+
+def softmax(logits, visible, v):
+    """out [B, n_q, H, d], lse [B, H, n_q], and sum_j p_j |v_j| of every output."""
+    lg = np.where(visible, logits, -np.inf)
+    top = np.max(lg, -1, initial=-np.inf, keepdims=True)
+    p = np.exp(lg - np.where(np.isfinite(top), top, 0.0))
+    total = p.sum(-1, keepdims=True)
+    with np.errstate(divide="ignore"):
+        lse = (np.where(np.isfinite(top), top, 0.0) + np.log(total))[..., 0]
+    p /= np.where(total > 0, total, 1.0)
+    t = lambda x: x.transpose(0, 2, 1, 3)  # noqa: E731
+    return t(np.matmul(p, v)), lse, t(np.matmul(p, np.abs(v)))
+
+
+def tolerances(q, k, n, r, dtype):
+    """(bound of an output relative to sum p |v|, bound of the lse error beside
+    2^-24 of its size). A logit errs by its fp32 sum, (d + r + 8) 2^-24 of its terms'
+    magnitude, and in BF16 by the coefficients' term with q U_r rounded to the other
+    side of a tie: 2^-8 of it, at most 2^-8 (the term is below 1 on these streams). A
+    weight errs by that and its rounding (2^-8 in BF16), once in O and once in the
+    sum; the fp32 sums over n keys by n 2^-24 each; the result rounds once more."""
+    d = q.shape[-1]
+    qk = np.matmul(np.abs(q).transpose(0, 2, 1, 3), np.abs(k).transpose(0, 1, 3, 2)).max() / np.sqrt(d) if k.shape[2] else 0.0
+    bf = dtype == "bf16"
+    dl = (d + r + 8) * 2.0 ** -24 * qk + (2.0 ** -8 if bf and r else 0.0)
+    return 2 * (dl + n * 2.0 ** -24) + (3 * 2.0 ** -8 if bf else 2.0 ** -22), dl + n * 2.0 ** -24 + (2.0 ** -8 if bf else 0.0)
+
+
+def check(got, glse, ref, rlse, mag, tol):
+    rel, ltol = tol
+    got, glse = got.double().cpu().numpy(), glse.double().cpu().numpy()
+    seen = np.isfinite(rlse)
+    assert np.array_equal(np.isneginf(glse), ~seen)
+    err = np.abs(got - ref) - rel * mag
+    assert (err <= 0).all(), (err.max(), np.unravel_index(err.argmax(), err.shape))
+    lerr = np.abs(glse[seen] - rlse[seen]) - 2.0 ** -22 * np.abs(rlse[seen]) - ltol
+    assert (lerr <= 0).all(), lerr.max()
