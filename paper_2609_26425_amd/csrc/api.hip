@@ -515,7 +515,7 @@ static qwm::AttendArgs attend_args(const quantwm_config* cfg, const void* calib,
   a.part_ml = nullptr;
   a.q_row0 = 0;
   a.windowed = 0;
-  a.n_sink = a.window = 0;
+  a.n_sink = a.window = a.chunks_per_part = 0;
   return a;
 }
 
@@ -577,6 +577,20 @@ static quantwm_status attend_common(const quantwm_config* cfg, const void* calib
     a.n_sink = window->n_sink < n_cache + n_act ? window->n_sink : n_cache + n_act;
     a.window = window->window;
   }
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (window && qwm::attend_few_takes(*cfg, n_q)) {
+    if (workspace && (reinterpret_cast<uintptr_t>(workspace) & 255))
+      return fail(QWM_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    int most = 1;
+    const int planes = qwm::attend_few_planes(n_q, cfg->heads, cfg->batch, n_cache + n_act, device_cus());
+    while (workspace && most < planes && planes_bytes(cfg, most + 1, n_q) <= workspace_bytes) ++most;
+    if (qwm::attend_few_plan(a, cfg->batch, device_cus(), most)) {
+      if (a.n_split > 1) set_planes(cfg, a, a.n_split, workspace);
+      const hipError_t e = qwm::launch_attend_few(a, cfg->head_dim, cfg->batch, s);
+      if (e != hipSuccess) return hip_fail(e, "attend launch");
+      return ok();
+    }
+  }
   if (!logits_out && workspace) {
     if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(QWM_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     // the cheapest number of parts that the workspace holds
@@ -587,7 +601,6 @@ static quantwm_status attend_common(const quantwm_config* cfg, const void* calib
     if (ns > 1) set_planes(cfg, a, ns, workspace);
   }
   a.q_row0 = logits_out ? q_first : 0;
-  hipStream_t s = static_cast<hipStream_t>(stream);
   if ((n_q + 255) / 256 * int64_t(a.n_split) > 0x7fffffff) return fail(QWM_ERR_UNSUPPORTED, "n_q too large");
   // the kernel keeps Query and key positions in 32 bits
   if (n_q > kMaxPositions || n_cache + n_act > kMaxPositions)
@@ -636,7 +649,10 @@ size_t quantwm_attend_window_workspace_bytes(const quantwm_config* cfg, int64_t 
   if (check_cfg(cfg) != QWM_OK || n_cache < 0 || n_act < 0 || n_q <= 0 || frame_tokens < 1) return 0;
   if (check_window(n_sink, window) != QWM_OK) return 0;
   const Window w = window_of(n_sink, window);
-  return attend_split_bytes(cfg, keys_in_reach(n_cache + n_act, frame_tokens, &w), n_q, nullptr);
+  const size_t split = attend_split_bytes(cfg, keys_in_reach(n_cache + n_act, frame_tokens, &w), n_q, nullptr);
+  if (!qwm::attend_few_takes(*cfg, n_q)) return split;
+  const size_t few = planes_bytes(cfg, qwm::attend_few_planes(n_q, cfg->heads, cfg->batch, n_cache + n_act, device_cus()), n_q);
+  return few > split ? few : split;
 }
 
 quantwm_status quantwm_attend_window(const quantwm_config* cfg, const void* calibs, int32_t n_epochs,
@@ -653,19 +669,26 @@ quantwm_status quantwm_attend_window(const quantwm_config* cfg, const void* cali
 // Key splits of the two passes of quantwm_attend_shared (0: no keys, no pass) and
 // the bytes of each one's partial planes.
 struct SharedPlan {
-  int prefix, own;
+  int prefix, own;              // planes
+  bool few_prefix, few_own;     // by the few-row kernel, in at most that many parts
   size_t prefix_bytes, own_bytes;
 };
 static SharedPlan shared_plan(const quantwm_config* prefix_cfg, int64_t n_prefix, const quantwm_config* cfg,
                               int64_t n_own, int64_t n_q) {
-  SharedPlan p{0, 0, 0, 0};
+  SharedPlan p{};
   const int cus = device_cus(), elem = qwm::elem_bytes(*cfg);
+  auto planes = [&](const quantwm_config* c, int64_t rows, int64_t n_keys, bool& few) {
+    const int ns = qwm::attend_splits(rows, c->heads, c->batch, n_keys, cus, elem);
+    few = qwm::attend_few_takes(*c, rows);
+    const int nf = few ? qwm::attend_few_planes(rows, c->heads, c->batch, n_keys, cus) : 0;
+    return nf > ns ? nf : ns;
+  };
   if (n_prefix > 0) {
-    p.prefix = qwm::attend_splits(n_q * cfg->batch, cfg->heads, 1, n_prefix, cus, elem);
+    p.prefix = planes(prefix_cfg, n_q * cfg->batch, n_prefix, p.few_prefix);
     p.prefix_bytes = size_t(qwm::align256(int64_t(planes_bytes(prefix_cfg, p.prefix, n_q * cfg->batch))));
   }
   if (n_own > 0) {
-    p.own = qwm::attend_splits(n_q, cfg->heads, cfg->batch, n_own, cus, elem);
+    p.own = planes(cfg, n_q, n_own, p.few_own);
     p.own_bytes = planes_bytes(cfg, p.own, n_q);
   }
   return p;
@@ -730,21 +753,30 @@ quantwm_status quantwm_attend_shared(const quantwm_config* prefix_cfg, const voi
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e;
+  // one pass: its partial planes at `at`
+  auto pass = [&](const quantwm_config* f, qwm::AttendArgs& a, bool few, int planes, int64_t n_keys, void* at) {
+    if (few && qwm::attend_few_plan(a, f->batch, device_cus(), planes)) {
+      set_planes(f, a, a.n_split, at);
+      return qwm::launch_attend_few(a, f->head_dim, f->batch, s);
+    }
+    set_planes(f, a, qwm::attend_splits(a.n_q, f->heads, f->batch, n_keys, device_cus(), qwm::elem_bytes(*f)), at);
+    return launch_attend(f, a, false, s);
+  };
   qwm::SharedArgs c{};
   c.n_q = n_q; c.heads = cfg->heads; c.batch = cfg->batch; c.out = out; c.lse = lse_out;
   if (p.prefix > 0) {
     qwm::AttendArgs a = attend_args(prefix_cfg, prefix_calibs, n_epochs, epoch_start, prefix_cache, n_prefix, nullptr,
                                     nullptr, 0, q, n_q * cfg->batch, n_prefix, 1, nullptr, nullptr, nullptr);
-    set_planes(prefix_cfg, a, p.prefix, workspace);
-    if ((e = launch_attend(prefix_cfg, a, false, s)) != hipSuccess) return hip_fail(e, "attend launch (prefix)");
-    c.prefix_o = a.part_o; c.prefix_ml = a.part_ml; c.n_prefix = p.prefix;
+    if ((e = pass(prefix_cfg, a, p.few_prefix, p.prefix, n_prefix, workspace)) != hipSuccess)
+      return hip_fail(e, "attend launch (prefix)");
+    c.prefix_o = a.part_o; c.prefix_ml = a.part_ml; c.n_prefix = a.n_split;
   }
   if (p.own > 0) {
     qwm::AttendArgs a = attend_args(cfg, calib, 1, nullptr, cache, n_cache, k_act, v_act, n_act, q, n_q,
                                     q_start - n_prefix, frame_tokens, nullptr, nullptr, nullptr);
-    set_planes(cfg, a, p.own, static_cast<uint8_t*>(workspace) + p.prefix_bytes);
-    if ((e = launch_attend(cfg, a, false, s)) != hipSuccess) return hip_fail(e, "attend launch (own keys)");
-    c.own_o = a.part_o; c.own_ml = a.part_ml; c.n_own = p.own;
+    if ((e = pass(cfg, a, p.few_own, p.own, n_own, static_cast<uint8_t*>(workspace) + p.prefix_bytes)) != hipSuccess)
+      return hip_fail(e, "attend launch (own keys)");
+    c.own_o = a.part_o; c.own_ml = a.part_ml; c.n_own = a.n_split;
   }
   if ((e = qwm::launch_shared_combine(c, cfg->head_dim, cfg->dtype == QWM_BF16, s)) != hipSuccess)
     return hip_fail(e, "shared combine launch");

@@ -2,6 +2,7 @@
 // to the kernel instances (one translation unit per element type, head_dim
 // and PSAC rank padding) and the log-sum-exp merge of partial results.
 #include "attend_shape.h"
+#include "few_shape.h"
 
 namespace qwm {
 namespace {
@@ -108,6 +109,13 @@ hipError_t launch_shared_combine_t(const SharedArgs& a, int d, hipStream_t s) {
 }
 
 template <typename T, int D>
+hipError_t launch_combine(const AttendArgs& a, int batch, hipStream_t s) {
+  hipLaunchKernelGGL((attend_combine<T, D>), dim3((unsigned)((a.n_q + 3) / 4), (unsigned)a.heads, (unsigned)batch),
+                     dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
 hipError_t launch_d(const AttendArgs& a, int batch, bool logits, hipStream_t s) {
   hipError_t e;
   if (a.rank == 0) e = launch_attend_rp<T, D, 0>(a, batch, logits, s);
@@ -115,12 +123,80 @@ hipError_t launch_d(const AttendArgs& a, int batch, bool logits, hipStream_t s) 
   else e = launch_attend_rp<T, D, 32>(a, batch, logits, s);
   // planes without an output: the caller joins them with others
   if (e != hipSuccess || logits || a.n_split == 1 || !a.out) return e;
-  hipLaunchKernelGGL((attend_combine<T, D>), dim3((unsigned)((a.n_q + 3) / 4), (unsigned)a.heads, (unsigned)batch),
-                     dim3(256), 0, s, a);
-  return hipGetLastError();
+  return launch_combine<T, D>(a, batch, s);
+}
+
+template <int D>
+hipError_t launch_few_d(const AttendArgs& a, int batch, hipStream_t s) {
+  hipError_t e;
+  if (a.rank == 0) e = launch_attend_few_rp<D, 0>(a, batch, s);
+  else if (a.rank <= 16) e = launch_attend_few_rp<D, 16>(a, batch, s);
+  else e = launch_attend_few_rp<D, 32>(a, batch, s);
+  if (e != hipSuccess || a.n_split == 1 || !a.out) return e;
+  return launch_combine<bf16, D>(a, batch, s);
+}
+
+// Parts that few_parts workgroups take for chunks_per_part = cpp: the most of any
+// Query block.
+int few_parts(const AttendArgs& a, int64_t cpp, int64_t* chunks) {
+  int64_t most = 0, total = 0;
+  for (int64_t qa = 0; qa < a.n_q; qa += kFewQ) {
+    const int64_t qb = qa + kFewQ < a.n_q ? qa + kFewQ : a.n_q;
+    const FewReach r = few_reach(a.q_start, a.frame_tokens, a.n_cache + a.n_act, a.n_sink, a.window, a.windowed != 0, qa, qb);
+    int64_t parts = 0, sum = 0;
+    for (int i = 0; i <= a.n_epochs; ++i) {
+      if (i == a.n_epochs && a.n_act == 0) break;
+      const int64_t c = few_segment_of(a, i, r).chunks;
+      parts += (c + cpp - 1) / cpp;
+      sum += c;
+    }
+    most = parts > most ? parts : most;
+    total = sum > total ? sum : total;
+  }
+  if (chunks) *chunks = total;
+  return int(most);
+}
+
+// Parts a launch asks for: one workgroup per CU, and at least a chunk for every wave.
+int64_t few_want(int64_t n_q, int heads, int batch, int64_t chunks, int cus) {
+  const int64_t wgs = (n_q + kFewQ - 1) / kFewQ * heads * batch, parts = cus / wgs, most = chunks / kFewWaves;
+  const int64_t w = parts < most ? parts : most;
+  return w > 1 ? w : 1;
 }
 
 }  // namespace
+
+bool attend_few_takes(const quantwm_config& c, int64_t n_q) {
+  return c.dtype == QWM_BF16 && !(c.storage & QWM_STORE_SPARSE) && n_q <= kFewRows;
+}
+
+int attend_few_planes(int64_t n_q, int heads, int batch, int64_t n_keys, int cus) {
+  // every segment (epoch) may end in a part of its own
+  return int(few_want(n_q, heads, batch, n_keys / kFewChunk + 2, cus)) + 16;
+}
+
+bool attend_few_plan(AttendArgs& a, int batch, int cus, int most) {
+  int64_t chunks = 0;
+  (void)few_parts(a, 1 << 30, &chunks);
+  const int64_t want = few_want(a.n_q, a.heads, batch, chunks, cus);
+  int64_t cpp = (chunks + want - 1) / want;
+  if (cpp < 1) cpp = 1;
+  int parts = few_parts(a, cpp, nullptr);
+  while (parts > most && cpp < chunks) {
+    cpp *= 2;
+    parts = few_parts(a, cpp, nullptr);
+  }
+  if (parts > most && parts > 1) return false;
+  a.chunks_per_part = cpp;
+  a.n_split = parts > 1 ? parts : 1;
+  return true;
+}
+
+hipError_t launch_attend_few(const AttendArgs& a, int d, int batch, hipStream_t s) {
+  if (d == 64) return launch_few_d<64>(a, batch, s);
+  if (d == 128) return launch_few_d<128>(a, batch, s);
+  return hipErrorInvalidValue;
+}
 
 hipError_t launch_shared_combine(const SharedArgs& a, int d, bool bf16_out, hipStream_t s) {
   return bf16_out ? launch_shared_combine_t<bf16>(a, d, s) : launch_shared_combine_t<float>(a, d, s);

@@ -46,4 +46,8 @@ constexpr size_t kLdsLimit = 160 * 1024;
 template <typename T, int D, int RP>
 hipError_t launch_attend_rp(const AttendArgs& a, int batch, bool logits, hipStream_t s);
 
+// The few-row kernel (BF16), one instance per head_dim and PSAC rank padding.
+template <int D, int RP>
+hipError_t launch_attend_few_rp(const AttendArgs& a, int batch, hipStream_t s);
+
 }  // namespace qwm

@@ -1,0 +1,60 @@
+// Key ranges of the few-row attention kernel, as the host counts them for its grid and
+// the kernel walks them: the 32-key chunks of one segment (an epoch's packed keys, or
+// the exact chunk) that a block of Queries may see.
+#pragma once
+
+#include "qwm_common.h"
+
+namespace qwm {
+
+constexpr int kFewQ = 32;      // Queries per workgroup: one matrix-core tile
+constexpr int kFewChunk = 32;  // keys per wave and step
+constexpr int kFewWaves = 8;
+
+struct FewSegment {
+  int64_t lo, hi, base, chunks;  // keys [lo, hi) in chunks from key `base`
+  int64_t cut, skip;             // after `cut` chunks, `skip` chunks in nobody's reach are left out
+};
+
+// Keys of Queries [qa, qb) of a launch: [0, kend), of which [0, ns) and [wlo, kend) are
+// in reach; below kfull and from wfull on every one of these Queries sees them.
+struct FewReach {
+  int64_t kend, kfull, ns, wlo, wfull;
+};
+
+inline __host__ __device__ FewReach few_reach(int64_t q_start, int64_t F, int64_t nc, int64_t n_sink, int64_t window,
+                                              bool windowed, int64_t qa, int64_t qb) {
+  FewReach r;
+  const int64_t first = q_start + (qa / F + 1) * F, last = q_start + ((qb - 1) / F + 1) * F;
+  r.kfull = first < nc ? first : nc;
+  r.kend = last < nc ? last : nc;
+  r.ns = windowed ? n_sink : 0;
+  const int64_t a = windowed ? first - window : 0, b = windowed ? last - window : 0;
+  r.wlo = a < 0 ? 0 : (a < nc ? a : nc);
+  r.wfull = b < 0 ? 0 : (b < nc ? b : nc);
+  return r;
+}
+
+inline __host__ __device__ FewSegment few_segment(int64_t lo, int64_t end, bool act, const FewReach& r) {
+  FewSegment s;
+  s.lo = lo;
+  s.hi = end < r.kend ? end : r.kend;
+  s.base = act ? lo : lo / kFewChunk * kFewChunk;
+  const int64_t all = s.hi > lo ? (s.hi - s.base + kFewChunk - 1) / kFewChunk : 0;
+  const int64_t sink = r.ns > lo ? (r.ns - s.base + kFewChunk - 1) / kFewChunk : 0;
+  s.cut = sink < all ? sink : all;
+  const int64_t from = r.wlo >= s.hi ? all : (r.wlo > s.base ? (r.wlo - s.base) / kFewChunk : 0);
+  s.skip = from > s.cut ? from - s.cut : 0;
+  s.chunks = all - s.skip;
+  return s;
+}
+
+// Segment i of a launch (n_epochs: the exact chunk).
+inline __host__ __device__ FewSegment few_segment_of(const AttendArgs& a, int i, const FewReach& r) {
+  const bool act = i == a.n_epochs;
+  const int64_t lo = act ? a.n_cache : a.epoch_start[i];
+  const int64_t end = act ? a.n_cache + a.n_act : (i + 1 < a.n_epochs ? a.epoch_start[i + 1] : a.n_cache);
+  return few_segment(lo, end, act, r);
+}
+
+}  // namespace qwm

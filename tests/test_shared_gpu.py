@@ -25,6 +25,8 @@ CASES = {
     "rows-before-own-keys": (2, 2, 128, "bf16", ([0], 400, 16, 32, 8, 0), (0, 90, 16, 32, 8, 0), 30, 0, 90),
     "one-prefix-key": (3, 2, 128, "bf16", ([0], 1, 16, 32, 8, 0), (0, 3, 16, 32, 8, 0), 1, 0, 3),
     "long-prefix": (16, 2, 64, "bf16", ([0, 5000], 9000, 64, 32, 8, 0), (20, 0, 16, 32, 8, 0), 1, 20, 2),
+    "few-frames": (3, 2, 128, "bf16", ([0, 100, 300], 900, 64, 16, 13, 1), (200, 40, 100, 64, 32, 0), 10, 220, 20),
+    "few-own": (9, 2, 64, "bf16", ([0], 500, 64, 32, 16, 0), (100, 11, 16, 32, 7, 1), 1, 100, 11),
     "f32": (3, 2, 64, "f32", ([0, 99], 700, 16, 32, 4, 0), (70, 33, 16, 32, 4, 0), 1, 70, 33),
     "f32-128": (2, 2, 128, "f32", ([0], 200, 16, 32, 32, 1), (65, 0, 16, 16, 8, 0), 20, 45, 40),
 }

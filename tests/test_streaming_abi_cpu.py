@@ -97,10 +97,14 @@ def test_shared_sizes():
     pcfg, cfg = _cfg(capacity=1 << 20), _cfg(batch=3)
     ws = qw.quantwm_attend_shared_workspace_bytes
     assert _shared(n_q=0) == qw.OK
-    plane = lambda rows: (rows * 128 * 4 + 255) // 256 * 256 + rows * 8  # noqa: E731
-    # short parts take one plane each: 3 x 2 x 4 rows
-    assert ws(pcfg, 64, cfg, 64, 0, 4) == (plane(24) + 255) // 256 * 256 + plane(24)
-    assert ws(pcfg, 0, cfg, 64, 0, 4) == plane(24) and ws(pcfg, 64, cfg, 0, 0, 4) == (plane(24) + 255) // 256 * 256
+    up = lambda x: (x + 255) // 256 * 256  # noqa: E731
+    rows = 3 * 2 * 4  # of one plane: running maxima, sums and 128 channels each
+    prefix, mine = ws(pcfg, 64, cfg, 0, 0, 4), ws(pcfg, 0, cfg, 64, 0, 4)
+    assert prefix >= rows * 130 * 4 and mine >= rows * 130 * 4 and prefix % 256 == 0
+    assert ws(pcfg, 64, cfg, 64, 0, 4) == prefix + mine == ws(pcfg, 64, cfg, 60, 4, 4)
+    # many rows: one plane a part once the launch fills the GPU
+    big = 3 * 2 * 50_000
+    assert ws(pcfg, 64, cfg, 0, 0, 50_000) == up(up(big * 128 * 4) + big * 8)
     assert ws(pcfg, 0, cfg, 0, 0, 4) == ws(pcfg, 64, cfg, 64, 0, 0) == 0
     assert ws(_cfg(batch=2), 64, cfg, 64, 0, 4) == 0 and ws(pcfg, -1, cfg, 64, 0, 4) == 0
 

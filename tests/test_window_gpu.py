@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 import torch
 
+import oracle
 import stream64 as s64
 from paper_2609_26425_amd import quantwm as qw
 
@@ -50,9 +51,26 @@ def _bounds(q_start, n_q, frame, n_sink, window, n):
     return hi, visible
 
 
-@pytest.mark.parametrize("name", list(CASES))
+# the same with 96 Queries and fewer, where another kernel runs (BF16); first its own shapes:
+# group sizes against a lane's channels, ranks that are no multiple of four, many parts
+FEW = {
+    "g16": (2, [0], 1000, 40, 0, 128, 16, 13, 16, 1, 40, 700, 900, 96, "bf16"),
+    "g16-i8": (1, [0, 333], 1000, 0, 1, 128, 100, 16, 16, 1, 40, 700, 900, 90, "bf16"),
+    "g64": (1, [0], 900, 31, 0, 64, 16, 7, 64, 3, 40, 500, 850, 64, "bf16"),
+    "g64-i8": (1, [0], 900, 33, 1, 128, 256, 30, 64, 3, 1000, 0, 850, 33, "bf16"),
+    "g32-64": (3, [0, 64, 200], 700, 0, 1, 64, 200, 20, 32, 1, 0, 1 << 50, 600, 65, "bf16"),
+    "g16-64": (1, [0], 700, 0, 0, 64, 30, 4, 16, 1, 33, 31, 600, 97, "bf16"),
+    "many-epochs": (1, [66 * i for i in range(40)], 2700, 20, 0, 64, 8, 4, 16, 5, 70, 2000, 2600, 30, "bf16"),
+    "long": (1, [0], 30_000, 100, 0, 64, 32, 8, 32, 1, 500, 20_000, 30_050, 3, "bf16"),
+}
+SHORT = {f"{k}-{m}": v[:13] + (min(m, v[13]), v[14]) for k, v in CASES.items() if v[14] == "bf16" and v[13] > 1
+         for m in (2, 45)}
+
+
+@pytest.mark.parametrize("name", list(CASES) + list(FEW) + list(SHORT))
 def test_window(name):
-    B, starts, n_pk, n_act, st, d, kc, r, g, frame, n_sink, window, q_start, n_q, dtype = CASES[name]
+    B, starts, n_pk, n_act, st, d, kc, r, g, frame, n_sink, window, q_start, n_q, dtype = \
+        {**CASES, **FEW, **SHORT}[name]
     H, n = 2, n_pk + n_act
     rng = np.random.default_rng(n + d + n_sink % 1000)
     p = s64.Packed(rng, B, H, d, kc, g, r, dtype, st, starts, n_pk)
@@ -111,8 +129,9 @@ def _calibrated(cfg, gen, blocks=1):
 
 @pytest.mark.parametrize("d,r,dtype", [(64, 4, "bf16"), (128, 6, "bf16"), (128, 32, "bf16"), (64, 13, "f32")])
 def test_window_over_sparse_rows(d, r, dtype):
-    """Sparse and slot-addressed PSAC rows give the same bits through a window."""
-    H, n, nq, starts = 3, 1200, 70, [0, 90, 500, 800]
+    """Sparse and slot-addressed PSAC rows give the same bits through a window (with more
+    than 96 Queries, where one kernel serves both)."""
+    H, n, nq, starts = 3, 1200, 120, [0, 90, 500, 800]
     gen = torch.Generator(device=DEV).manual_seed(d + r)
     got = []
     cfgs = [qw.make_config(1, H, d, 16, 32, r, 4, n, dtype, st, coef_stage=n) for st in (0, 4)]
@@ -134,11 +153,12 @@ def test_window_over_sparse_rows(d, r, dtype):
         assert torch.equal(got[i][0], got[2 + i][0]) and torch.equal(got[i][1], got[2 + i][1]), i
 
 
+@pytest.mark.parametrize("nq", [40, 120])
 @pytest.mark.parametrize("dtype,st", [("bf16", 0), ("bf16", 1), ("f32", 0)])
-def test_tiles_out_of_reach_are_not_read(dtype, st):
+def test_tiles_out_of_reach_are_not_read(dtype, st, nq):
     """Slots between the sinks' last tile and the window's first one, and past the
     cached tokens, may hold anything (bytes 0xff: NaN scales)."""
-    n, nq, n_sink, window = 1500, 40, 70, 200
+    n, n_sink, window = 1500, 70, 200
     gen = torch.Generator(device=DEV).manual_seed(3)
     cfg = qw.make_config(1, 2, 128, 16, 32, 8, 4, 1600, dtype, st)
     calibs, _, _ = _calibrated(cfg, gen)
@@ -154,6 +174,34 @@ def test_tiles_out_of_reach_are_not_read(dtype, st):
         got.append((out, lse))
     assert torch.isfinite(got[0][0].float()).all()
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+@pytest.mark.parametrize("st", [0, 1])
+def test_neighbour_epochs_of_other_magnitude(st):
+    """An epoch boundary inside a chunk, Values around 2^-100 on one side and steps near
+    the largest binary16 on the other, few Queries: neither side's keys reach the
+    other's Queries as an infinity or weight."""
+    H, d, kc, nq, starts, n = 2, 128, 16, 60, [0, 100, 200], 300
+    scale = [2.0 ** -100, 2.0 ** 14, 2.0 ** -100]
+    rng = np.random.default_rng(st)
+    p = s64.Packed(rng, 1, H, d, kc, 32, 4, "bf16", st, [0], n)  # Keys and formats; Values and tables below
+    p.tables, p.starts = [], starts
+    for e, vs in enumerate(scale):
+        k, v = s64.rounded(rng.standard_normal((1, 100, H, d)), "bf16"), s64.rounded(vs * rng.uniform(-1.5, 1.5, (1, 100, H, d)), "bf16")
+        mu = [s64.rounded(x * rng.standard_normal((1, H, kc, d)), "bf16") for x in (1.0, vs * 2.0 ** -6)]
+        u = np.stack([np.linalg.qr(rng.standard_normal((d, d)))[0][:4] for _ in range(H)])[None]
+        p.tables.append((*mu, np.ones((1, H, d), np.float32), s64.rounded(u, "bf16"), np.ones((1, H, 4), np.float32)))
+        oracle.append(p.ocfg, p.tables[e], p.cache, starts[e], k, v)
+    q = s64.rounded(rng.standard_normal((1, nq, H, d)), "bf16")
+    k, v = p.keys_values()
+    # 20 rows a frame: frame 0 sees epoch 0, frames 1 and 2 windows of one epoch each and its neighbours' last keys
+    hi = 100 + 20 * (np.arange(nq) // 20)
+    visible = (np.arange(n) < hi[:, None]) & (np.arange(n) >= hi[:, None] - 100)
+    ref, rlse, mag = s64.softmax(p.logits(q), visible, v)
+    qd = s64.dev(q, torch.bfloat16)
+    out, lse = torch.full_like(qd, 7.0), torch.empty(1, H, nq, device=DEV)
+    qw.quantwm_attend_window(p.cfg, p.blocks(), starts, p.on_device(), n, None, None, 0, qd, nq, 80, 20, 0, 100, out, lse)
+    s64.check(out, lse, ref, rlse, mag, s64.tolerances(q, k, n, 4, "bf16"))
 
 
 def test_a_window_of_everything_is_attention_over_epochs():
