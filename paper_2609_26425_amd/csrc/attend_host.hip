@@ -167,7 +167,7 @@ int64_t few_want(int64_t n_q, int heads, int batch, int64_t chunks, int cus) {
 }  // namespace
 
 bool attend_few_takes(const quantwm_config& c, int64_t n_q) {
-  return c.dtype == QWM_BF16 && !(c.storage & QWM_STORE_SPARSE) && n_q <= kFewRows;
+  return c.dtype == QWM_BF16 && !(c.storage & QWM_STORE_SPARSE) && c.rank % 4 == 0 && n_q <= kFewRows;
 }
 
 int attend_few_planes(int64_t n_q, int heads, int batch, int64_t n_keys, int cus) {

@@ -66,13 +66,36 @@ class Packed:
                         k[b, h, lo:hi], v[b, h, lo:hi] = rounded(dk[lo:hi], self.dtype), rounded(dv[lo:hi], self.dtype)
         return k, v
 
-    def logits(self, q):
-        """Every Query against every packed key, [B, H, n_q, n], in 64 bits."""
+    def logits(self, q, few=False):
+        """Every Query against every packed key, [B, H, n_q, n], in 64 bits. The Keys as
+        the kernels hold them: rounded to the element type, or (few) as they decode.
+        q U_r and the coefficients are rounded to it in both."""
         if self.n == 0:
             return np.zeros((self.batch, self.heads, q.shape[1], 0))
-        _, _, lg = oracle.attend(self.ocfg, None, self.cache, self.n, q, self.n, 1, want_logits=True,
-                                 epochs=list(zip(self.starts, self.tables)))
-        return lg.reshape(self.batch, self.heads, q.shape[1], self.n)
+        if not few:
+            _, _, lg = oracle.attend(self.ocfg, None, self.cache, self.n, q, self.n, 1, want_logits=True,
+                                     epochs=list(zip(self.starts, self.tables)))
+            return lg.reshape(self.batch, self.heads, q.shape[1], self.n)
+        out = np.zeros((self.batch, self.heads, q.shape[1], self.n))
+        for b in range(self.batch):
+            for h in range(self.heads):
+                qh = q[b, :, h].astype(np.float64)
+                for lo, hi, t in zip(self.starts, self.starts[1:] + [self.n], self.tables):
+                    if hi > lo:
+                        k0, c, _ = oracle.decode(self.ocfg, t, self.cache, b, h, hi)
+                        qu = rounded(qh @ t[3][b, h].astype(np.float64).T, self.dtype).astype(np.float64)
+                        out[b, h, :, lo:hi] = qh @ k0[lo:hi].T + qu @ rounded(c[lo:hi], self.dtype).astype(np.float64).T
+        return out / np.sqrt(self.d)
+
+    def residuals(self):
+        """What the codes add to the Keys' centroids, [B, H, n, d]."""
+        out = np.zeros((self.batch, self.heads, self.n, self.d))
+        none = tuple(np.zeros_like(x) for x in self.tables[0][:2])
+        for b in range(self.batch):
+            for h in range(self.heads):
+                if self.n:
+                    out[b, h] = oracle.decode(self.ocfg, none, self.cache, b, h, self.n)[0]
+        return out
 
 
 def exact_logits(q, k_act):
@@ -94,18 +117,28 @@ def softmax(logits, visible, v):
     return t(np.matmul(p, v)), lse, t(np.matmul(p, np.abs(v)))
 
 
-def tolerances(q, k, n, r, dtype):
+def tolerances(q, k, n, r, dtype, res=None):
     """(bound of an output relative to sum p |v|, bound of the lse error beside
     2^-24 of its size). A logit errs by its fp32 sum, (d + r + 8) 2^-24 of its terms'
     magnitude, and in BF16 by the coefficients' term with q U_r rounded to the other
     side of a tie: 2^-8 of it, at most 2^-8 (the term is below 1 on these streams). A
     weight errs by that and its rounding (2^-8 in BF16), once in O and once in the
-    sum; the fp32 sums over n keys by n 2^-24 each; the result rounds once more."""
+    sum; the fp32 sums over n keys by n 2^-24 each; the result rounds once more. res: the
+    residuals s (code - z), where they are binary16 operands: 2^-11 of their part of a
+    logit."""
     d = q.shape[-1]
     qk = np.matmul(np.abs(q).transpose(0, 2, 1, 3), np.abs(k).transpose(0, 1, 3, 2)).max() / np.sqrt(d) if k.shape[2] else 0.0
     bf = dtype == "bf16"
     dl = (d + r + 8) * 2.0 ** -24 * qk + (2.0 ** -8 if bf and r else 0.0)
+    if res is not None and res.shape[2]:
+        dl += 2.0 ** -11 * np.matmul(np.abs(q).transpose(0, 2, 1, 3), np.abs(res).transpose(0, 1, 3, 2)).max() / np.sqrt(d)
     return 2 * (dl + n * 2.0 ** -24) + (3 * 2.0 ** -8 if bf else 2.0 ** -22), dl + n * 2.0 ** -24 + (2.0 ** -8 if bf else 0.0)
+
+
+def rebuilt(dtype, n_q, r):
+    """Whether a launch rounds rebuilt Keys to the element type: not with up to 64 BF16
+    rows a head and coefficient rows of whole words."""
+    return dtype != "bf16" or n_q > 64 or r % 4 != 0
 
 
 def check(got, glse, ref, rlse, mag, tol):

@@ -43,20 +43,23 @@ def test_shared(name):
     q = s64.rounded(rng.standard_normal((B, n_q, H, d)), dtype)
     pk, pv = pre.keys_values()
     k, v = own.keys_values()
-    logits = own.logits(q)
+    few_own, few_pre = (not s64.rebuilt(dtype, m, x) for m, x in ((n_q, r), (B * n_q, pr)))
+    logits = own.logits(q, few_own)
     ka = va = None
     if n_act:
         ka, va = (s64.rounded(rng.standard_normal((B, n_act, H, d)), dtype) for _ in range(2))
         k, v = (np.concatenate([x, y.transpose(0, 2, 1, 3)], 2) for x, y in ((k, ka), (v, va)))
         logits = np.concatenate([logits, s64.exact_logits(q, ka)], 3)
-    shared = pre.logits(q.reshape(1, B * n_q, H, d)).reshape(H, B, n_q, n_pre).transpose(1, 0, 2, 3)
+    flat = q.reshape(1, B * n_q, H, d)
+    shared = pre.logits(flat, few_pre).reshape(H, B, n_q, n_pre).transpose(1, 0, 2, 3)
     logits = np.concatenate([shared, logits], 3)
     k, v = (np.concatenate([np.repeat(x, B, 0), y], 2) for x, y in ((pk, k), (pv, v)))
     n, q_start = n_pre + n_pk + n_act, n_pre + first
     visible = np.arange(n) < (q_start + (np.arange(n_q) // frame + 1) * frame)[:, None]
     ref, rlse, mag = s64.softmax(logits, visible, v)
     # the join adds the weights of the parts: n 2^-24 more covers its exponentials and sums
-    tol = s64.tolerances(q, k, 2 * n + 64, max(r, pr), dtype)
+    tol = [max(x) for x in zip(s64.tolerances(q, k, 2 * n + 64, max(r, pr), dtype, own.residuals() if few_own else None),
+                               s64.tolerances(flat, pk, 2 * n + 64, max(r, pr), dtype, pre.residuals() if few_pre else None))]
     dt = own.cfg.torch_dtype
     nb = qw.quantwm_attend_shared_workspace_bytes(pre.cfg, n_pre, own.cfg, n_pk, n_act, n_q)
     assert (nb > 0) == (n > 0)
