@@ -1,7 +1,7 @@
 """Builds libquantwm.so (the gfx950 HIP kernels plus the C ABI) in-tree.
 
 Translation units compile in parallel: append.hip (fp32) and append_bf16.hip
-once per (head_dim, group size), attend.hip once per (element type, head_dim, PSAC rank padding), attend_few.hip once per
+once per (head_dim, group size), attend.hip once per (element type, head_dim, PSAC rank padding), attend_few.hip and attend_few_f32.hip once per
 (head_dim, PSAC rank padding),
 attend_host.hip, rotary.hip, calib.hip, basis.hip, coef.hip and api.hip; the objects link into ``paper_2609_26425_amd/libquantwm.so``.
 """
@@ -49,6 +49,8 @@ def _units():
     for d in (64, 128):
         for rp in (0, 16, 32):
             units.append((f"attend_few_{d}_r{rp}.o", "attend_few.hip",
+                          ["-fno-honor-nans", f"-DQWM_ATTEND_D={d}", f"-DQWM_ATTEND_RP={rp}"]))
+            units.append((f"attend_few_f32_{d}_r{rp}.o", "attend_few_f32.hip",
                           ["-fno-honor-nans", f"-DQWM_ATTEND_D={d}", f"-DQWM_ATTEND_RP={rp}"]))
     units.append(("attend_host.o", "attend_host.hip", ["-fno-honor-nans"]))
     for name in ("rotary", "calib", "basis", "coef", "api"):

@@ -582,11 +582,11 @@ static quantwm_status attend_common(const quantwm_config* cfg, const void* calib
     if (workspace && (reinterpret_cast<uintptr_t>(workspace) & 255))
       return fail(QWM_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     int most = 1;
-    const int planes = qwm::attend_few_planes(n_q, cfg->heads, cfg->batch, n_cache + n_act, device_cus());
+    const int planes = qwm::attend_few_planes(n_q, cfg->heads, cfg->batch, n_cache + n_act, device_cus(), qwm::elem_bytes(*cfg));
     while (workspace && most < planes && planes_bytes(cfg, most + 1, n_q) <= workspace_bytes) ++most;
-    if (qwm::attend_few_plan(a, cfg->batch, device_cus(), most)) {
+    if (qwm::attend_few_plan(a, cfg->batch, device_cus(), qwm::elem_bytes(*cfg), most)) {
       if (a.n_split > 1) set_planes(cfg, a, a.n_split, workspace);
-      const hipError_t e = qwm::launch_attend_few(a, cfg->head_dim, cfg->batch, s);
+      const hipError_t e = qwm::launch_attend_few(a, cfg->head_dim, qwm::elem_bytes(*cfg), cfg->batch, s);
       if (e != hipSuccess) return hip_fail(e, "attend launch");
       return ok();
     }
@@ -651,7 +651,8 @@ size_t quantwm_attend_window_workspace_bytes(const quantwm_config* cfg, int64_t 
   const Window w = window_of(n_sink, window);
   const size_t split = attend_split_bytes(cfg, keys_in_reach(n_cache + n_act, frame_tokens, &w), n_q, nullptr);
   if (!qwm::attend_few_takes(*cfg, n_q)) return split;
-  const size_t few = planes_bytes(cfg, qwm::attend_few_planes(n_q, cfg->heads, cfg->batch, n_cache + n_act, device_cus()), n_q);
+  const size_t few = planes_bytes(cfg, qwm::attend_few_planes(n_q, cfg->heads, cfg->batch, n_cache + n_act, device_cus(),
+                                                                 qwm::elem_bytes(*cfg)), n_q);
   return few > split ? few : split;
 }
 
@@ -680,7 +681,7 @@ static SharedPlan shared_plan(const quantwm_config* prefix_cfg, int64_t n_prefix
   auto planes = [&](const quantwm_config* c, int64_t rows, int64_t n_keys, bool& few) {
     const int ns = qwm::attend_splits(rows, c->heads, c->batch, n_keys, cus, elem);
     few = qwm::attend_few_takes(*c, rows);
-    const int nf = few ? qwm::attend_few_planes(rows, c->heads, c->batch, n_keys, cus) : 0;
+    const int nf = few ? qwm::attend_few_planes(rows, c->heads, c->batch, n_keys, cus, elem) : 0;
     return nf > ns ? nf : ns;
   };
   if (n_prefix > 0) {
@@ -755,9 +756,9 @@ quantwm_status quantwm_attend_shared(const quantwm_config* prefix_cfg, const voi
   hipError_t e;
   // one pass: its partial planes at `at`
   auto pass = [&](const quantwm_config* f, qwm::AttendArgs& a, bool few, int planes, int64_t n_keys, void* at) {
-    if (few && qwm::attend_few_plan(a, f->batch, device_cus(), planes)) {
+    if (few && qwm::attend_few_plan(a, f->batch, device_cus(), qwm::elem_bytes(*f), planes)) {
       set_planes(f, a, a.n_split, at);
-      return qwm::launch_attend_few(a, f->head_dim, f->batch, s);
+      return qwm::launch_attend_few(a, f->head_dim, qwm::elem_bytes(*f), f->batch, s);
     }
     set_planes(f, a, qwm::attend_splits(a.n_q, f->heads, f->batch, n_keys, device_cus(), qwm::elem_bytes(*f)), at);
     return launch_attend(f, a, false, s);

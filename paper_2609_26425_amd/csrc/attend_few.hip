@@ -82,32 +82,12 @@ __global__ __launch_bounds__(64 * few_waves(TAB)) void attend_few_kernel(const A
   const int64_t nc = a.n_cache + a.n_act, F = a.frame_tokens;
   const FewReach reach = few_reach(a.q_start, F, nc, a.n_sink, a.window, a.windowed != 0, qa, qb);
 
-  // ---- the segment of this part: a lane counts for each epoch
-  const int64_t cpp = a.chunks_per_part;
-  int seg = 0;
   int64_t before = 0;
-  if (a.n_epochs == 1) {
-    const int p0 = int((few_segment_of(a, 0, reach).chunks + cpp - 1) / cpp);
-    if (part >= p0) {
-      seg = 1;
-      before = p0;
-    }
-  } else {
-    static_assert(kMaxEpochs == 64, "a lane per epoch");
-    int past = lane < a.n_epochs ? int((few_segment_of(a, lane, reach).chunks + cpp - 1) / cpp) : 0;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(past, o);
-      past += lane >= o ? y : 0;
-    }
-    const uint64_t at = __ballot(past > part);
-    seg = at ? __builtin_ctzll(at) : a.n_epochs;
-    before = seg > 0 ? __builtin_amdgcn_readlane(past, seg - 1) : 0;
-  }
+  const int seg = few_segment_at(a, reach, part, lane, before);
   const bool act = seg == a.n_epochs;
   FewSegment g{};
   if (!act || a.n_act > 0) g = few_segment_of(a, seg, reach);
-  const int64_t t0 = (part - before) * cpp, t1 = t0 + cpp < g.chunks ? t0 + cpp : g.chunks;
+  const int64_t cpp = a.chunks_per_part, t0 = (part - before) * cpp, t1 = t0 + cpp < g.chunks ? t0 + cpp : g.chunks;
   float* plane_ml = a.part_ml ? a.part_ml + 2 * ((int64_t(part) * a.heads * gridDim.z + bh) * a.n_q + qa) : nullptr;
   if (t0 >= t1 && a.part_o) {  // this block of Queries has fewer parts than another: an empty plane
     if (threadIdx.x < rows) {

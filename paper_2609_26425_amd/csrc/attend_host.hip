@@ -127,6 +127,16 @@ hipError_t launch_d(const AttendArgs& a, int batch, bool logits, hipStream_t s) 
 }
 
 template <int D>
+hipError_t launch_few_f32_d(const AttendArgs& a, int batch, hipStream_t s) {
+  hipError_t e;
+  if (a.rank == 0) e = launch_attend_few_f32_rp<D, 0>(a, batch, s);
+  else if (a.rank <= 16) e = launch_attend_few_f32_rp<D, 16>(a, batch, s);
+  else e = launch_attend_few_f32_rp<D, 32>(a, batch, s);
+  if (e != hipSuccess || a.n_split == 1 || !a.out) return e;
+  return launch_combine<float, D>(a, batch, s);
+}
+
+template <int D>
 hipError_t launch_few_d(const AttendArgs& a, int batch, hipStream_t s) {
   hipError_t e;
   if (a.rank == 0) e = launch_attend_few_rp<D, 0>(a, batch, s);
@@ -157,9 +167,11 @@ int few_parts(const AttendArgs& a, int64_t cpp, int64_t* chunks) {
   return int(most);
 }
 
-// Parts a launch asks for: one workgroup per CU, and at least a chunk for every wave.
-int64_t few_want(int64_t n_q, int heads, int batch, int64_t chunks, int cus) {
-  const int64_t wgs = (n_q + kFewQ - 1) / kFewQ * heads * batch, parts = cus / wgs, most = chunks / kFewWaves;
+// Parts a launch asks for: one workgroup per CU (fp32: two, of four waves), and at least
+// a chunk for every wave.
+int64_t few_want(int64_t n_q, int heads, int batch, int64_t chunks, int cus, int elem) {
+  const int64_t wgs = (n_q + kFewQ - 1) / kFewQ * heads * batch, parts = (elem == 4 ? 2 * cus : cus) / wgs,
+                most = chunks / (elem == 4 ? 4 : kFewWaves);
   const int64_t w = parts < most ? parts : most;
   return w > 1 ? w : 1;
 }
@@ -167,18 +179,21 @@ int64_t few_want(int64_t n_q, int heads, int batch, int64_t chunks, int cus) {
 }  // namespace
 
 bool attend_few_takes(const quantwm_config& c, int64_t n_q) {
-  return c.dtype == QWM_BF16 && !(c.storage & QWM_STORE_SPARSE) && c.rank % 4 == 0 && n_q <= kFewRows;
+  if (c.storage & QWM_STORE_SPARSE) return false;
+  // BF16: up to two blocks of rows, with coefficient rows of whole words
+  if (c.dtype == QWM_BF16) return c.rank % 4 == 0 && n_q <= 64;
+  return n_q <= 2048;
 }
 
-int attend_few_planes(int64_t n_q, int heads, int batch, int64_t n_keys, int cus) {
+int attend_few_planes(int64_t n_q, int heads, int batch, int64_t n_keys, int cus, int elem) {
   // every segment (epoch) may end in a part of its own
-  return int(few_want(n_q, heads, batch, n_keys / kFewChunk + 2, cus)) + 16;
+  return int(few_want(n_q, heads, batch, n_keys / kFewChunk + 2, cus, elem)) + 16;
 }
 
-bool attend_few_plan(AttendArgs& a, int batch, int cus, int most) {
+bool attend_few_plan(AttendArgs& a, int batch, int cus, int elem, int most) {
   int64_t chunks = 0;
   (void)few_parts(a, 1 << 30, &chunks);
-  const int64_t want = few_want(a.n_q, a.heads, batch, chunks, cus);
+  const int64_t want = few_want(a.n_q, a.heads, batch, chunks, cus, elem);
   int64_t cpp = (chunks + want - 1) / want;
   if (cpp < 1) cpp = 1;
   int parts = few_parts(a, cpp, nullptr);
@@ -192,7 +207,12 @@ bool attend_few_plan(AttendArgs& a, int batch, int cus, int most) {
   return true;
 }
 
-hipError_t launch_attend_few(const AttendArgs& a, int d, int batch, hipStream_t s) {
+hipError_t launch_attend_few(const AttendArgs& a, int d, int elem, int batch, hipStream_t s) {
+  if (elem == 4) {
+    if (d == 64) return launch_few_f32_d<64>(a, batch, s);
+    if (d == 128) return launch_few_f32_d<128>(a, batch, s);
+    return hipErrorInvalidValue;
+  }
   if (d == 64) return launch_few_d<64>(a, batch, s);
   if (d == 128) return launch_few_d<128>(a, batch, s);
   return hipErrorInvalidValue;

@@ -49,5 +49,7 @@ hipError_t launch_attend_rp(const AttendArgs& a, int batch, bool logits, hipStre
 // The few-row kernel (BF16), one instance per head_dim and PSAC rank padding.
 template <int D, int RP>
 hipError_t launch_attend_few_rp(const AttendArgs& a, int batch, hipStream_t s);
+template <int D, int RP>
+hipError_t launch_attend_few_f32_rp(const AttendArgs& a, int batch, hipStream_t s);
 
 }  // namespace qwm

@@ -57,4 +57,29 @@ inline __host__ __device__ FewSegment few_segment_of(const AttendArgs& a, int i,
   return few_segment(lo, end, act, r);
 }
 
+#ifdef __HIPCC__
+// The segment of part `part`, and the parts before it: a lane counts for each epoch.
+__device__ inline int few_segment_at(const AttendArgs& a, const FewReach& r, int part, int lane, int64_t& before) {
+  static_assert(kMaxEpochs == 64, "a lane per epoch");
+  const int64_t cpp = a.chunks_per_part;
+  before = 0;
+  if (a.n_epochs == 1) {
+    const int p0 = int((few_segment_of(a, 0, r).chunks + cpp - 1) / cpp);
+    if (part < p0) return 0;
+    before = p0;
+    return 1;
+  }
+  int past = lane < a.n_epochs ? int((few_segment_of(a, lane, r).chunks + cpp - 1) / cpp) : 0;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(past, o);
+    past += lane >= o ? y : 0;
+  }
+  const uint64_t at = __ballot(past > part);
+  const int seg = at ? __builtin_ctzll(at) : a.n_epochs;
+  before = seg > 0 ? __builtin_amdgcn_readlane(past, seg - 1) : 0;
+  return seg;
+}
+#endif
+
 }  // namespace qwm

@@ -196,15 +196,13 @@ template <int D, int G>
 hipError_t launch_append_bf16(const AppendArgs& a, int batch, hipStream_t s);
 hipError_t launch_attend_f32(const AttendArgs& a, int d, int batch, bool logits, hipStream_t s);
 hipError_t launch_attend_bf16(const AttendArgs& a, int d, int batch, bool logits, hipStream_t s);
-// The few-row kernel: Query blocks of 32 rows whose key range is cut into parts, for
-// launches of at most kFewRows Query rows per (b, h) in BF16, with slot-addressed
-// coefficient rows of whole words. Sets a's parts: at most `most`
-// (false: the key segments in reach alone are more).
-constexpr int64_t kFewRows = 64;
+// The few-row kernels: Query blocks of 32 rows whose key range is cut into parts, for
+// small launches over slot-addressed coefficient rows. attend_few_plan sets a's parts:
+// at most `most` (false: the key segments in reach alone are more).
 bool attend_few_takes(const quantwm_config& c, int64_t n_q);
-int attend_few_planes(int64_t n_q, int heads, int batch, int64_t n_keys, int cus);
-bool attend_few_plan(AttendArgs& a, int batch, int cus, int most);
-hipError_t launch_attend_few(const AttendArgs& a, int d, int batch, hipStream_t s);
+int attend_few_planes(int64_t n_q, int heads, int batch, int64_t n_keys, int cus, int elem);
+bool attend_few_plan(AttendArgs& a, int batch, int cus, int elem, int most);
+hipError_t launch_attend_few(const AttendArgs& a, int d, int elem, int batch, hipStream_t s);
 hipError_t launch_shared_combine(const SharedArgs& a, int d, bool bf16_out, hipStream_t s);
 hipError_t launch_rotary(const RotaryArgs& a, int d, bool bf16_data, bool halves, hipStream_t s);
 size_t attend_lds_bytes(int d, int elem, int rank, int n_centroids, bool tables_in_lds);

@@ -264,34 +264,59 @@ def quantwm_attend_epochs_workspace_bytes(cfg, epoch_start, n_cache, n_act, n_q)
                                                           n_act, n_q))
 
 
-def _check_tensors(dtype, **sized):
-    """Refuses, before a pointer is taken, tensors of another type, too small for
-    the call, or on another device than the one it runs on. sized: name -> (tensor
-    or None, least number of elements, dtype or None for the call's)."""
-    for name, (t, least, dt) in sized.items():
-        if t is None:
-            continue
-        if not isinstance(t, torch.Tensor):
-            raise TypeError(f"{name}: expected a torch.Tensor or None")
-        if t.dtype != (dt or dtype):
-            raise ValueError(f"{name}: expected {dt or dtype}, got {t.dtype}")
-        if t.numel() < least:
-            raise ValueError(f"{name}: {t.numel()} elements, the call needs {least}")
-        if torch.cuda.is_available() and (not t.is_cuda or t.device.index != torch.cuda.current_device()):
-            raise ValueError(f"{name}: on {t.device}, the call runs on cuda:{torch.cuda.current_device()}")
+# The calls below are made once per layer and step, on launches of a few microseconds:
+# each argument is checked and turned into an address in one small call.
+_gpu = None
 
 
-def _ws_bytes(workspace):
-    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+def _device():
+    """Index of the device that a call runs on (None in a process without a GPU)."""
+    global _gpu
+    if _gpu is None:
+        _gpu = torch.cuda.is_available()
+    return torch.cuda.current_device() if _gpu else None
 
 
-def _attend_tensors(cfg, calib, blocks, cache, k_act, v_act, n_act, q, n_q, out, lse_out):
-    row = cfg.heads * cfg.head_dim
-    _check_tensors(cfg.torch_dtype, k_act=(k_act, cfg.batch * n_act * row, None),
-                   v_act=(v_act, cfg.batch * n_act * row, None), q=(q, cfg.batch * n_q * row, None),
-                   out=(out, cfg.batch * n_q * row, None), lse_out=(lse_out, cfg.batch * cfg.heads * n_q, torch.float32),
-                   calib=(calib, blocks * quantwm_calib_bytes(cfg), torch.uint8),
-                   cache=(cache, quantwm_cache_bytes(cfg), torch.uint8))
+def _address(name, t, dtype, least, dev):
+    """The device address of a tensor (0 for None). Refuses one of another type, too
+    small for the call, with gaps, or on another device than the call's."""
+    if t is None:
+        return 0
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor or None")
+    if dtype is not None and t.dtype is not dtype:
+        raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.numel() < least:
+        raise ValueError(f"{name}: {t.numel()} elements, the call needs {least}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: tensors must be contiguous")
+    if dev is not None and t.get_device() != dev:
+        raise ValueError(f"{name}: on {t.device}, the call runs on cuda:{dev}")
+    return t.data_ptr()
+
+
+def _raw_stream(stream, dev):
+    if stream is None:
+        return None if dev is None else torch._C._cuda_getCurrentRawStream(dev)
+    return _stream(stream)
+
+
+_block_bytes = {}
+
+
+def _sizes(cfg):
+    """(calibration block bytes, cache bytes) of a configuration, by its value."""
+    key = bytes(cfg)
+    got = _block_bytes.get(key)
+    if got is None:
+        if len(_block_bytes) >= 256:
+            _block_bytes.clear()
+        got = _block_bytes[key] = (quantwm_calib_bytes(cfg), quantwm_cache_bytes(cfg))
+    return got
+
+
+def _starts(epoch_start):
+    return (ctypes.c_int64 * len(epoch_start))(*epoch_start)
 
 
 def quantwm_attend_window(cfg, calibs, epoch_start, cache, n_cache, k_act, v_act, n_act, q, n_q, q_start,
@@ -299,13 +324,18 @@ def quantwm_attend_window(cfg, calibs, epoch_start, cache, n_cache, k_act, v_act
     """Attention over the first n_sink keys and the last `window` positions up to the
     end of the Query's frame. calibs: one device buffer of len(epoch_start)
     calibration blocks; epoch_start: host ints, [0] for a single block."""
-    starts = (ctypes.c_int64 * len(epoch_start))(*[int(x) for x in epoch_start])
-    _attend_tensors(cfg, calibs, len(epoch_start), cache, k_act, v_act, n_act, q, n_q, out, lse_out)
-    _check_tensors(torch.uint8, workspace=(workspace, 0, workspace.dtype if workspace is not None else None))
-    _check(_lib.quantwm_attend_window(ctypes.byref(cfg), _ptr(calibs), len(epoch_start), starts, _ptr(cache), n_cache,
-                                      _ptr(k_act), _ptr(v_act), n_act, _ptr(q), n_q, q_start, frame_tokens, n_sink,
-                                      window, _ptr(out), _ptr(lse_out), _ptr(workspace), _ws_bytes(workspace),
-                                      _stream(stream)))
+    dev, dt, u8 = _device(), cfg.torch_dtype, torch.uint8
+    row, (block, slots) = cfg.batch * cfg.heads * cfg.head_dim, _sizes(cfg)
+    status = _lib.quantwm_attend_window(
+        cfg, _address("calibs", calibs, u8, len(epoch_start) * block, dev), len(epoch_start), _starts(epoch_start),
+        _address("cache", cache, u8, slots, dev), n_cache, _address("k_act", k_act, dt, n_act * row, dev),
+        _address("v_act", v_act, dt, n_act * row, dev), n_act, _address("q", q, dt, n_q * row, dev), n_q, q_start,
+        frame_tokens, n_sink, window, _address("out", out, dt, n_q * row, dev),
+        _address("lse_out", lse_out, torch.float32, cfg.batch * cfg.heads * n_q, dev),
+        _address("workspace", workspace, None, 0, dev), 0 if workspace is None else workspace.nbytes,
+        _raw_stream(stream, dev))
+    if status:
+        _check(status)
 
 
 def quantwm_attend_window_workspace_bytes(cfg, n_cache, n_act, n_q, frame_tokens, n_sink, window) -> int:
@@ -319,16 +349,19 @@ def quantwm_attend_shared(prefix_cfg, prefix_calibs, epoch_start, prefix_cache, 
     """Attention of cfg.batch rollouts over [one shared prefix | own packed keys |
     own exact keys]. prefix_calibs: len(epoch_start) calibration blocks of
     prefix_cfg; workspace: quantwm_attend_shared_workspace_bytes() bytes."""
-    starts = (ctypes.c_int64 * len(epoch_start))(*[int(x) for x in epoch_start])
-    _attend_tensors(cfg, calib, 1, cache, k_act, v_act, n_act, q, n_q, out, lse_out)
-    _check_tensors(torch.uint8, workspace=(workspace, 0, workspace.dtype if workspace is not None else None),
-                   prefix_calibs=(prefix_calibs, len(epoch_start) * quantwm_calib_bytes(prefix_cfg), None),
-                   prefix_cache=(prefix_cache, quantwm_cache_bytes(prefix_cfg), None))
-    _check(_lib.quantwm_attend_shared(ctypes.byref(prefix_cfg), _ptr(prefix_calibs), len(epoch_start), starts,
-                                      _ptr(prefix_cache), n_prefix, ctypes.byref(cfg), _ptr(calib), _ptr(cache),
-                                      n_cache, _ptr(k_act), _ptr(v_act), n_act, _ptr(q), n_q, q_start, frame_tokens,
-                                      _ptr(out), _ptr(lse_out), _ptr(workspace), _ws_bytes(workspace),
-                                      _stream(stream)))
+    dev, dt, u8 = _device(), cfg.torch_dtype, torch.uint8
+    row, (block, slots), (pblock, pslots) = cfg.batch * cfg.heads * cfg.head_dim, _sizes(cfg), _sizes(prefix_cfg)
+    status = _lib.quantwm_attend_shared(
+        prefix_cfg, _address("prefix_calibs", prefix_calibs, u8, len(epoch_start) * pblock, dev), len(epoch_start),
+        _starts(epoch_start), _address("prefix_cache", prefix_cache, u8, pslots, dev), n_prefix, cfg,
+        _address("calib", calib, u8, block, dev), _address("cache", cache, u8, slots, dev), n_cache,
+        _address("k_act", k_act, dt, n_act * row, dev), _address("v_act", v_act, dt, n_act * row, dev), n_act,
+        _address("q", q, dt, n_q * row, dev), n_q, q_start, frame_tokens, _address("out", out, dt, n_q * row, dev),
+        _address("lse_out", lse_out, torch.float32, cfg.batch * cfg.heads * n_q, dev),
+        _address("workspace", workspace, None, 0, dev), 0 if workspace is None else workspace.nbytes,
+        _raw_stream(stream, dev))
+    if status:
+        _check(status)
 
 
 def quantwm_attend_shared_workspace_bytes(prefix_cfg, n_prefix, cfg, n_cache, n_act, n_q) -> int:
@@ -356,21 +389,21 @@ def rotary_axes(cfg, dims, height, width, base=10000.0, pairs=ROTARY_ADJACENT, f
     return out
 
 
-def _token_rows(cfg, name, t, n):
-    """Elements from one token to the next of a [B, n, H, d] tensor whose tokens may
-    lie apart (a slice of a fused projection)."""
-    shape = (cfg.batch, n, cfg.heads, cfg.head_dim)
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
-    row = cfg.heads * cfg.head_dim
-    if n * cfg.batch <= 1:
-        step = row
-    else:
-        step = t.stride(1) if n > 1 else t.stride(0)
-    inner = (cfg.heads == 1 or t.stride(2) == cfg.head_dim) and t.stride(3) == 1
-    if not inner or (cfg.batch > 1 and t.stride(0) != n * step):
+def _token_rows(cfg, name, t, n, dev):
+    """(address, elements from one token to the next) of a [B, n, H, d] tensor whose
+    tokens may lie apart (a slice of a fused projection)."""
+    B, H, d = cfg.batch, cfg.heads, cfg.head_dim
+    if t.shape != (B, n, H, d):
+        raise ValueError(f"{name}: expected shape {(B, n, H, d)}, got {tuple(t.shape)}")
+    if t.dtype is not cfg.torch_dtype:
+        raise ValueError(f"{name}: expected {cfg.torch_dtype}, got {t.dtype}")
+    if dev is not None and t.get_device() != dev:
+        raise ValueError(f"{name}: on {t.device}, the call runs on cuda:{dev}")
+    s0, s1, s2, s3 = t.stride()
+    step = s1 if n > 1 else (s0 if B > 1 else H * d)
+    if s3 != 1 or (H > 1 and s2 != d) or (B > 1 and s0 != n * step):
         raise ValueError(f"{name}: heads and channels must be contiguous and the tokens evenly spaced")
-    return step
+    return t.data_ptr(), step
 
 
 def quantwm_rotary(cfg, axes, q, k, n, q_out, k_out=None, pos0=0, pos=None, inverse=False, stream=None):
@@ -379,15 +412,18 @@ def quantwm_rotary(cfg, axes, q, k, n, q_out, k_out=None, pos0=0, pos=None, inve
     int32). inverse: the transpose, which is the gradient."""
     if n == 0:
         return
-    row = cfg.heads * cfg.head_dim
-    _check_tensors(cfg.torch_dtype, q=(q, 0, None), k=(k, 0, None), q_out=(q_out, cfg.batch * n * row, None),
-                   k_out=(k_out, cfg.batch * n * row, None), pos=(pos, cfg.batch * n * 3, torch.int32))
-    step = _token_rows(cfg, "q", q, n)
-    if k is not None and _token_rows(cfg, "k", k, n) != step:
-        raise ValueError("q and k must have the same token stride")
-    _check(_lib.quantwm_rotary(ctypes.byref(cfg), ctypes.byref(axes), pos0, _ptr(pos),
-                               ctypes.c_void_p(q.data_ptr()), None if k is None else ctypes.c_void_p(k.data_ptr()), n,
-                               step, _ptr(q_out), _ptr(k_out), int(inverse), _stream(stream)))
+    dev, dt, size = _device(), cfg.torch_dtype, cfg.batch * n * cfg.heads * cfg.head_dim
+    qp, step = _token_rows(cfg, "q", q, n, dev)
+    kp = 0
+    if k is not None:
+        kp, kstep = _token_rows(cfg, "k", k, n, dev)
+        if kstep != step:
+            raise ValueError("q and k must have the same token stride")
+    status = _lib.quantwm_rotary(cfg, axes, pos0, _address("pos", pos, torch.int32, cfg.batch * n * 3, dev), qp, kp, n,
+                                 step, _address("q_out", q_out, dt, size, dev), _address("k_out", k_out, dt, size, dev),
+                                 bool(inverse), _raw_stream(stream, dev))
+    if status:
+        _check(status)
 
 
 ATTEND_NOALLOC_SCRATCH_BYTES = 128 << 20  # QWM_ATTEND_NOALLOC_SCRATCH_BYTES

@@ -132,9 +132,9 @@ def _calibrated(cfg, gen, blocks=1):
 
 @pytest.mark.parametrize("d,r,dtype", [(64, 4, "bf16"), (128, 6, "bf16"), (128, 32, "bf16"), (64, 13, "f32")])
 def test_window_over_sparse_rows(d, r, dtype):
-    """Sparse and slot-addressed PSAC rows give the same bits through a window (with more
-    than 64 Queries, where one kernel serves both)."""
-    H, n, nq, starts = 3, 1200, 120, [0, 90, 500, 800]
+    """Sparse and slot-addressed PSAC rows give the same bits through a window (with so
+    many Queries that one kernel serves both)."""
+    H, n, nq, starts = 3, 1200, 120 if dtype == "bf16" else 2100, [0, 90, 500, 800]
     gen = torch.Generator(device=DEV).manual_seed(d + r)
     got = []
     cfgs = [qw.make_config(1, H, d, 16, 32, r, 4, n, dtype, st, coef_stage=n) for st in (0, 4)]
