@@ -516,6 +516,7 @@ static qwm::AttendArgs attend_args(const quantwm_config* cfg, const void* calib,
   a.q_row0 = 0;
   a.windowed = 0;
   a.n_sink = a.window = a.chunks_per_part = 0;
+  a.q_blocks = a.block_rows = 0;
   return a;
 }
 

@@ -11,7 +11,6 @@
 #include "attend_device.h"
 #include "attend_shape.h"
 #include "few_shape.h"
-#include "xcd_order.h"
 
 #include <atomic>
 
@@ -41,42 +40,33 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_few_f32_kernel(const At
   const int Kc = a.n_centroids, r = a.rank, G = D / a.L.ng;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32,
             hf = lane / 32;
-  uint32_t bx, by, bz;
-  {
-    const uint32_t gx = gridDim.x, gy = gridDim.y, n = gx * gy * gridDim.z;
-    const uint32_t task = qwm_xcd_task(blockIdx.x + gx * (blockIdx.y + gy * blockIdx.z), n);
-    bx = task % gx;
-    by = (task / gx) % gy;
-    bz = task / (gx * gy);
-  }
-  const int h = int(by), b = int(bz);
-  const int64_t bh = int64_t(b) * a.heads + h;
-  const int part = int(bx) % a.n_split;
-  const int64_t qa = int64_t(bx / a.n_split) * kFewQ, qb = qa + kFewQ < a.n_q ? qa + kFewQ : a.n_q;
-  const int rows = int(qb - qa);
-  const int64_t nc = a.n_cache + a.n_act, F = a.frame_tokens;
-  const FewReach reach = few_reach(a.q_start, F, nc, a.n_sink, a.window, a.windowed != 0, qa, qb);
-  int64_t before = 0;
+  const int part = int(blockIdx.x), h = int(blockIdx.y), b = int(blockIdx.z / uint32_t(a.q_blocks));
+  const int64_t bh = int64_t(b) * a.heads + h, n_bh = int64_t(a.heads) * (gridDim.z / uint32_t(a.q_blocks));
+  const int qa = int(blockIdx.z % uint32_t(a.q_blocks)) * kFewQ, rows = min(kFewQ, int(a.n_q) - qa);
+  const int64_t nc = a.n_cache + a.n_act;
+  const uint32_t F = uint32_t(a.frame_tokens);
+  const FewReach reach = few_reach(a.q_start, F, nc, a.n_sink, a.window, a.windowed != 0, uint32_t(qa), uint32_t(qa + rows));
+  int before = 0;
   const int seg = few_segment_at(a, reach, part, lane, before);
   const bool act = seg == a.n_epochs;
   FewSegment g{};
   if (!act || a.n_act > 0) g = few_segment_of(a, seg, reach);
-  const int64_t cpp = a.chunks_per_part, t0 = (part - before) * cpp, t1 = t0 + cpp < g.chunks ? t0 + cpp : g.chunks;
-  float* plane_ml = a.part_ml ? a.part_ml + 2 * ((int64_t(part) * a.heads * gridDim.z + bh) * a.n_q + qa) : nullptr;
+  const int cpp = int(a.chunks_per_part), t0 = (part - before) * cpp, t1 = min(t0 + cpp, int(g.chunks));
+  float* plane_ml = a.part_ml ? a.part_ml + 2 * ((int64_t(part) * n_bh + bh) * a.n_q + qa) : nullptr;
   if (t0 >= t1 && a.part_o) {  // this block of Queries has fewer parts than another: an empty plane
-    if (threadIdx.x < rows) {
+    if (int(threadIdx.x) < rows) {
       plane_ml[2 * threadIdx.x] = -__builtin_inff();
       plane_ml[2 * threadIdx.x + 1] = 0.0f;
     }
     return;
   }
-  auto key_of = [&](int64_t t) __attribute__((always_inline)) { return g.base + (t >= g.cut ? t + g.skip : t) * CK; };
+  auto key_of = [&](int t) __attribute__((always_inline)) { return int(g.base) + (t >= int(g.cut) ? t + int(g.skip) : t) * CK; };
 
   const uint8_t* slab = a.calib + int64_t(act ? 0 : seg) * a.calib_stride + bh * a.slab;
   const float* gK = reinterpret_cast<const float*>(slab + a.o_mu_k) + hf * HK;
   const float* gV = reinterpret_cast<const float*>(slab + a.o_mu_v) + hf * HK;
   float* vt = reinterpret_cast<float*>(smem_raw) + wave * FewTile<D>::FLOATS;
-  const int qi = int(qa) + l32;
+  const int qi = qa + l32;
   const bool qvalid = l32 < rows;
 
   // ---- packed fields: the loads hold no branch (see attend_few.hip)
@@ -96,8 +86,8 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_few_f32_kernel(const At
 #pragma unroll
   for (int u = 0; u < W; ++u) grp[u] = (hf * HK + 16 * u) / G;
   typedef F32Regs<W, RP> Regs;
-  auto load = [&](Regs& p, int64_t t) __attribute__((always_inline)) {
-    const int k0 = int(key_of(t));
+  auto load = [&](Regs& p, int t) __attribute__((always_inline)) {
+    const int k0 = key_of(t);
     auto codes = [&](auto rsrc, uint32_t (&to)[W]) __attribute__((always_inline)) {
       if constexpr (W == 4) {
         const auto c = __builtin_amdgcn_raw_buffer_load_b128(rsrc, l32 * (D / 4) + hf * (D / 8), k0 * (D / 4), 0);
@@ -180,19 +170,19 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_few_f32_kernel(const At
     for (int i = 0; i < 16; ++i) oacc[cb][i] = 0.0f;
   int lim = int(nc), wfrom = 0;
   {
-    const int64_t l = a.q_start + (qi / F + 1) * F, w = a.windowed ? l - a.window : 0;
+    const int64_t l = a.q_start + int64_t(uint32_t(qi) / F + 1) * F, w = a.windowed ? l - a.window : 0;
     lim = int(l < nc ? l : nc);
     wfrom = int(w < 0 ? 0 : (w < nc ? w : nc));
   }
   const float mscale = 1.4426950408889634f / sqrtf((float)D), tau = 8.0f / mscale;  // as in attend.hip
 
   // softmax of the logits s of one chunk and O^T += V^T P^T, with the Values in the tile
-  auto finish = [&](f32x16& s, int64_t k0) __attribute__((always_inline)) {
+  auto finish = [&](f32x16& s, int k0) __attribute__((always_inline)) {
     if (k0 < g.lo || k0 + CK > (reach.kfull < g.hi ? reach.kfull : g.hi) || (k0 + CK > reach.ns && k0 < reach.wfull)) {
       const int klo = int(g.lo), khi = int(g.hi) < lim ? int(g.hi) : lim;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int key = int(k0) + acc_row(i, hf);
+        const int key = k0 + acc_row(i, hf);
         if (key >= khi || key < klo || (key >= int(reach.ns) && key < wfrom)) s[i] = -__builtin_inff();
       }
     }
@@ -240,8 +230,8 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_few_f32_kernel(const At
       const float s = in ? (float)__builtin_bit_cast(_Float16, uint16_t(SI8 ? sg : sb)) : 0.0f;
       dequant_codes<16, SI8>(code, s, z, mu, x, f16x2{c, c});
     };
-    for (int64_t t = t0 + wave; t < t1; t += NW) {
-      const int64_t k0 = key_of(t);
+    for (int t = t0 + wave; t < t1; t += NW) {
+      const int k0 = key_of(t);
       const float* mk = gK + int64_t(int(P.k_id) < Kc ? int(P.k_id) : Kc - 1) * D;
       const float* mv = gV + int64_t(int(P.v_id) < Kc ? int(P.v_id) : Kc - 1) * D;
       const bool in = k0 + l32 >= g.lo;  // not a key of the neighbouring epoch before the segment's first
@@ -274,8 +264,9 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_few_f32_kernel(const At
   } else {
     // exact rows, the last one again past the end
     const int64_t last = a.n_act - 1;
-    for (int64_t t = t0 + wave; t < t1; t += NW) {
-      const int64_t k0 = key_of(t), i0 = k0 - a.n_cache + l32;
+    for (int t = t0 + wave; t < t1; t += NW) {
+      const int k0 = key_of(t);
+      const int64_t i0 = k0 - a.n_cache + l32;
       const int64_t at = ((int64_t(b) * a.n_act + (i0 < last ? i0 : last)) * a.heads + h) * D + hf * HK;
       const float4* kr = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.k_act) + at);
       const float4* vr = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.v_act) + at);
@@ -333,7 +324,7 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_few_f32_kernel(const At
       o += e * mo[(w * rows + row) * OS + c];
     }
     if (a.part_o) {
-      a.part_o[((int64_t(part) * a.heads * gridDim.z + bh) * a.n_q + qa + row) * D + c] = o;
+      a.part_o[((int64_t(part) * n_bh + bh) * a.n_q + qa + row) * D + c] = o;
       if (c == 0) {
         plane_ml[2 * row] = M;
         plane_ml[2 * row + 1] = l;
@@ -362,7 +353,7 @@ hipError_t launch_k(const AttendArgs& a, int batch, hipStream_t s) {
     if (e != hipSuccess) return e;
     raised.fetch_or(bit, std::memory_order_release);
   }
-  const dim3 grid((unsigned)((a.n_q + kFewQ - 1) / kFewQ * a.n_split), (unsigned)a.heads, (unsigned)batch);
+  const dim3 grid((unsigned)a.n_split, (unsigned)a.heads, (unsigned)(a.q_blocks * batch));
   hipLaunchKernelGGL((attend_few_f32_kernel<D, RP, SI8>), grid, dim3(64 * kF32Waves), lds, s, a);
   return hipGetLastError();
 }

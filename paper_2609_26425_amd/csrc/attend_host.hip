@@ -150,9 +150,10 @@ hipError_t launch_few_d(const AttendArgs& a, int batch, hipStream_t s) {
 // Query block.
 int few_parts(const AttendArgs& a, int64_t cpp, int64_t* chunks) {
   int64_t most = 0, total = 0;
-  for (int64_t qa = 0; qa < a.n_q; qa += kFewQ) {
-    const int64_t qb = qa + kFewQ < a.n_q ? qa + kFewQ : a.n_q;
-    const FewReach r = few_reach(a.q_start, a.frame_tokens, a.n_cache + a.n_act, a.n_sink, a.window, a.windowed != 0, qa, qb);
+  for (int64_t qa = 0; qa < a.n_q; qa += a.block_rows) {
+    const int64_t qb = qa + a.block_rows < a.n_q ? qa + a.block_rows : a.n_q;
+    const FewReach r = few_reach(a.q_start, uint32_t(a.frame_tokens), a.n_cache + a.n_act, a.n_sink, a.window,
+                                 a.windowed != 0, uint32_t(qa), uint32_t(qb));
     int64_t parts = 0, sum = 0;
     for (int i = 0; i <= a.n_epochs; ++i) {
       if (i == a.n_epochs && a.n_act == 0) break;
@@ -171,7 +172,7 @@ int few_parts(const AttendArgs& a, int64_t cpp, int64_t* chunks) {
 // a chunk for every wave.
 int64_t few_want(int64_t n_q, int heads, int batch, int64_t chunks, int cus, int elem) {
   const int64_t wgs = (n_q + kFewQ - 1) / kFewQ * heads * batch, parts = (elem == 4 ? 2 * cus : cus) / wgs,
-                most = chunks / (elem == 4 ? 4 : kFewWaves);
+                most = chunks / (elem == 4 ? 4 : 8);
   const int64_t w = parts < most ? parts : most;
   return w > 1 ? w : 1;
 }
@@ -191,6 +192,8 @@ int attend_few_planes(int64_t n_q, int heads, int batch, int64_t n_keys, int cus
 }
 
 bool attend_few_plan(AttendArgs& a, int batch, int cus, int elem, int most) {
+  a.block_rows = int(elem == 2 && a.n_q <= 16 ? a.n_q : (a.n_q < kFewQ ? a.n_q : kFewQ));
+  a.q_blocks = int((a.n_q + a.block_rows - 1) / a.block_rows);
   int64_t chunks = 0;
   (void)few_parts(a, 1 << 30, &chunks);
   const int64_t want = few_want(a.n_q, a.heads, batch, chunks, cus, elem);

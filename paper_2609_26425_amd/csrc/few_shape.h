@@ -7,9 +7,8 @@
 
 namespace qwm {
 
-constexpr int kFewQ = 32;      // Queries per workgroup: one matrix-core tile
+constexpr int kFewQ = 32;      // most Queries of a workgroup
 constexpr int kFewChunk = 32;  // keys per wave and step
-constexpr int kFewWaves = 8;
 
 struct FewSegment {
   int64_t lo, hi, base, chunks;  // keys [lo, hi) in chunks from key `base`
@@ -22,10 +21,11 @@ struct FewReach {
   int64_t kend, kfull, ns, wlo, wfull;
 };
 
-inline __host__ __device__ FewReach few_reach(int64_t q_start, int64_t F, int64_t nc, int64_t n_sink, int64_t window,
-                                              bool windowed, int64_t qa, int64_t qb) {
+inline __host__ __device__ FewReach few_reach(int64_t q_start, uint32_t F, int64_t nc, int64_t n_sink, int64_t window,
+                                              bool windowed, uint32_t qa, uint32_t qb) {
   FewReach r;
-  const int64_t first = q_start + (qa / F + 1) * F, last = q_start + ((qb - 1) / F + 1) * F;
+  // (32-bit quotients: a 64-bit one is some 150 instructions on the device)
+  const int64_t first = q_start + int64_t(qa / F + 1) * F, last = q_start + int64_t((qb - 1) / F + 1) * F;
   r.kfull = first < nc ? first : nc;
   r.kend = last < nc ? last : nc;
   r.ns = windowed ? n_sink : 0;
@@ -59,17 +59,17 @@ inline __host__ __device__ FewSegment few_segment_of(const AttendArgs& a, int i,
 
 #ifdef __HIPCC__
 // The segment of part `part`, and the parts before it: a lane counts for each epoch.
-__device__ inline int few_segment_at(const AttendArgs& a, const FewReach& r, int part, int lane, int64_t& before) {
+__device__ inline int few_segment_at(const AttendArgs& a, const FewReach& r, int part, int lane, int& before) {
   static_assert(kMaxEpochs == 64, "a lane per epoch");
-  const int64_t cpp = a.chunks_per_part;
+  const uint32_t cpp = uint32_t(a.chunks_per_part);
   before = 0;
   if (a.n_epochs == 1) {
-    const int p0 = int((few_segment_of(a, 0, r).chunks + cpp - 1) / cpp);
+    const int p0 = int((uint32_t(few_segment_of(a, 0, r).chunks) + cpp - 1) / cpp);
     if (part < p0) return 0;
     before = p0;
     return 1;
   }
-  int past = lane < a.n_epochs ? int((few_segment_of(a, lane, r).chunks + cpp - 1) / cpp) : 0;
+  int past = lane < a.n_epochs ? int((uint32_t(few_segment_of(a, lane, r).chunks) + cpp - 1) / cpp) : 0;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int y = __shfl_up(past, o);

@@ -150,7 +150,10 @@ struct AttendArgs {
   // its frame
   int windowed;
   int64_t n_sink, window;
-  int64_t chunks_per_part;  // few-row kernel only: 32-key chunks of a part (n_split parts a Query block)
+  // few-row kernels only: 32-key chunks of a part (n_split parts a Query block), blocks of
+  // block_rows Queries
+  int64_t chunks_per_part;
+  int q_blocks, block_rows;
 };
 
 // Joins the partial planes of attention over a shared prefix (one chunk of all
