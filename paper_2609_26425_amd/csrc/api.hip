@@ -579,7 +579,7 @@ static quantwm_status attend_common(const quantwm_config* cfg, const void* calib
     a.window = window->window;
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (window && qwm::attend_few_takes(*cfg, n_q)) {
+  if (window && qwm::attend_few_takes(*cfg, n_q, keys_in_reach(n_cache + n_act, frame_tokens, window))) {
     if (workspace && (reinterpret_cast<uintptr_t>(workspace) & 255))
       return fail(QWM_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     int most = 1;
@@ -651,7 +651,7 @@ size_t quantwm_attend_window_workspace_bytes(const quantwm_config* cfg, int64_t 
   if (check_window(n_sink, window) != QWM_OK) return 0;
   const Window w = window_of(n_sink, window);
   const size_t split = attend_split_bytes(cfg, keys_in_reach(n_cache + n_act, frame_tokens, &w), n_q, nullptr);
-  if (!qwm::attend_few_takes(*cfg, n_q)) return split;
+  if (!qwm::attend_few_takes(*cfg, n_q, keys_in_reach(n_cache + n_act, frame_tokens, &w))) return split;
   const size_t few = planes_bytes(cfg, qwm::attend_few_planes(n_q, cfg->heads, cfg->batch, n_cache + n_act, device_cus(),
                                                                  qwm::elem_bytes(*cfg)), n_q);
   return few > split ? few : split;
@@ -681,7 +681,7 @@ static SharedPlan shared_plan(const quantwm_config* prefix_cfg, int64_t n_prefix
   const int cus = device_cus(), elem = qwm::elem_bytes(*cfg);
   auto planes = [&](const quantwm_config* c, int64_t rows, int64_t n_keys, bool& few) {
     const int ns = qwm::attend_splits(rows, c->heads, c->batch, n_keys, cus, elem);
-    few = qwm::attend_few_takes(*c, rows);
+    few = qwm::attend_few_takes(*c, rows, n_keys);
     const int nf = few ? qwm::attend_few_planes(rows, c->heads, c->batch, n_keys, cus, elem) : 0;
     return nf > ns ? nf : ns;
   };

@@ -603,10 +603,13 @@ hipError_t launch_k(const AttendArgs& a, int batch, hipStream_t s) {
 
 template <int D, int G, int RP, int NQ>
 hipError_t launch_n(const AttendArgs& a, int batch, hipStream_t s) {
-  // the Value table is worth its staging once a part has as many keys as it has rows
-  const bool tab = a.chunks_per_part * kFewChunk >= int64_t(a.n_centroids);
-  if (a.L.i8) return tab ? launch_k<D, G, RP, NQ, true, true>(a, batch, s) : launch_k<D, G, RP, NQ, false, true>(a, batch, s);
-  return tab ? launch_k<D, G, RP, NQ, true, false>(a, batch, s) : launch_k<D, G, RP, NQ, false, false>(a, batch, s);
+  if constexpr (NQ == 1) {
+    // the Value table is worth its staging once a part has as many keys as it has rows
+    // (launches of more than 16 Queries are taken with thousands of keys)
+    if (a.chunks_per_part * kFewChunk < int64_t(a.n_centroids))
+      return a.L.i8 ? launch_k<D, G, RP, 1, false, true>(a, batch, s) : launch_k<D, G, RP, 1, false, false>(a, batch, s);
+  }
+  return a.L.i8 ? launch_k<D, G, RP, NQ, true, true>(a, batch, s) : launch_k<D, G, RP, NQ, true, false>(a, batch, s);
 }
 
 template <int D, int G, int RP>

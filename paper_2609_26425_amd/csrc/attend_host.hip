@@ -169,21 +169,29 @@ int few_parts(const AttendArgs& a, int64_t cpp, int64_t* chunks) {
 }
 
 // Parts a launch asks for: one workgroup per CU (fp32: two, of four waves), and at least
-// a chunk for every wave.
+// a chunk for every wave. Launches of one chunk a wave stay one part.
 int64_t few_want(int64_t n_q, int heads, int batch, int64_t chunks, int cus, int elem) {
   const int64_t wgs = (n_q + kFewQ - 1) / kFewQ * heads * batch, parts = (elem == 4 ? 2 * cus : cus) / wgs,
-                most = chunks / (elem == 4 ? 4 : 8);
+                most = chunks <= (elem == 4 ? 4 : 12) ? 1 : chunks / (elem == 4 ? 4 : 8);
   const int64_t w = parts < most ? parts : most;
   return w > 1 ? w : 1;
 }
 
 }  // namespace
 
-bool attend_few_takes(const quantwm_config& c, int64_t n_q) {
+bool attend_few_takes(const quantwm_config& c, int64_t n_q, int64_t n_keys) {
   if (c.storage & QWM_STORE_SPARSE) return false;
-  // BF16: up to two blocks of rows, with coefficient rows of whole words
-  if (c.dtype == QWM_BF16) return c.rank % 4 == 0 && n_q <= 64;
-  return n_q <= 2048;
+  // BF16: one block of rows, with coefficient rows of whole words, over enough keys that
+  // decoding them outweighs the merge of the waves' O rows (d = 128, 12 heads, us here /
+  // tiled: 1 Query x 300 keys 13 / 15, x 30,000 33 / 55; 16 x 1,000 20 / 18, x 8,000 27 / 28, x
+  // 30,000 37 / 56; 32 x 4,000 28 / 24, x 30,000 44 / 56; two blocks are never faster).
+  if (c.dtype == QWM_BF16) return c.rank % 4 == 0 && n_q <= kFewQ && n_keys >= 384 * (n_q - 1);
+  // fp32: up to about 16 (d = 128: 6) products of 32 Queries x 32 keys a SIMD; beyond, blocks of
+  // 256 rows decode less (d = 64, us here / tiled: 2 heads x 257 Queries x 362 keys 18 / 29; 8 x
+  // 512 x 3,000 59 / 61; 8 x 1,024 x 3,000 95 / 89. d = 128: 2 x 257 x 362 27 / 48, 2 x 1,024 x
+  // 3,000 82 / 92, 8 x 1,024 x 1,024 94 / 78).
+  const double units = double((n_q + kFewQ - 1) / kFewQ) * c.heads * c.batch * double((n_keys + kFewChunk - 1) / kFewChunk);
+  return n_q <= 4096 && units <= (c.head_dim == 64 ? 16384 : 6144);
 }
 
 int attend_few_planes(int64_t n_q, int heads, int batch, int64_t n_keys, int cus, int elem) {

@@ -202,7 +202,7 @@ hipError_t launch_attend_bf16(const AttendArgs& a, int d, int batch, bool logits
 // The few-row kernels: Query blocks of 32 rows whose key range is cut into parts, for
 // small launches over slot-addressed coefficient rows. attend_few_plan sets a's parts:
 // at most `most` (false: the key segments in reach alone are more).
-bool attend_few_takes(const quantwm_config& c, int64_t n_q);
+bool attend_few_takes(const quantwm_config& c, int64_t n_q, int64_t n_keys);
 int attend_few_planes(int64_t n_q, int heads, int batch, int64_t n_keys, int cus, int elem);
 bool attend_few_plan(AttendArgs& a, int batch, int cus, int elem, int most);
 hipError_t launch_attend_few(const AttendArgs& a, int d, int elem, int batch, hipStream_t s);

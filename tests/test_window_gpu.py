@@ -51,22 +51,29 @@ def _bounds(q_start, n_q, frame, n_sink, window, n):
     return hi, visible
 
 
-# the same with 64 Queries and fewer, where another kernel runs (BF16); first its own shapes:
-# group sizes against a lane's channels, ranks that are no multiple of four, many parts
+# the same with few Queries, where another kernel runs; first its own shapes: group sizes
+# against a lane's channels, ranks that are no multiple of four, many parts
 FEW = {
-    "g16": (2, [0], 1000, 40, 0, 128, 16, 12, 16, 1, 40, 700, 900, 64, "bf16"),
-    "g16-i8": (1, [0, 333], 1000, 0, 1, 128, 100, 16, 16, 1, 40, 700, 900, 61, "bf16"),
-    "g64": (1, [0], 900, 31, 0, 64, 16, 8, 64, 3, 40, 500, 850, 64, "bf16"),
-    "g64-i8": (1, [0], 900, 33, 1, 128, 256, 30, 64, 3, 1000, 0, 850, 33, "bf16"),
-    "g32-64": (3, [0, 64, 200], 700, 0, 1, 64, 200, 20, 32, 1, 0, 1 << 50, 600, 65, "bf16"),
-    "g16-64": (1, [0], 700, 0, 0, 64, 30, 4, 16, 1, 33, 31, 600, 97, "bf16"),
-    "g64-128": (1, [0], 900, 10, 0, 128, 60, 32, 64, 2, 10, 500, 850, 10, "bf16"),
-    "odd-rank": (1, [0], 900, 10, 0, 128, 60, 13, 32, 2, 10, 500, 850, 10, "bf16"),
-    "many-epochs": (1, [66 * i for i in range(40)], 2700, 20, 0, 64, 8, 4, 16, 5, 70, 2000, 2600, 30, "bf16"),
+    "g16": (2, [0], 2600, 40, 0, 128, 16, 12, 16, 1, 40, 2400, 2620, 7, "bf16"),
+    "g16-i8": (1, [0, 333], 6200, 0, 1, 128, 100, 16, 16, 1, 40, 5900, 6150, 16, "bf16"),
+    "g16-i8-32": (1, [0, 333], 12_000, 0, 1, 128, 100, 16, 16, 5, 11_990, 40, 11_950, 32, "bf16"),
+    "g32-i8-25": (1, [0], 9400, 30, 1, 128, 128, 32, 32, 1, 300, 9100, 9400, 25, "bf16"),
+    "g64": (1, [0], 7400, 31, 0, 64, 16, 8, 64, 3, 40, 7400, 7400, 20, "bf16"),
+    "g64-i8": (1, [0], 12_000, 33, 1, 64, 256, 28, 64, 3, 13_000, 0, 11_990, 32, "bf16"),
+    "g64-128": (1, [0], 6700, 10, 0, 128, 60, 32, 64, 2, 10, 6600, 6690, 18, "bf16"),
+    "g32-64": (1, [0, 64, 200, 3000], 6400, 0, 1, 64, 200, 20, 32, 1, 0, 1 << 50, 6380, 17, "bf16"),
+    "g16-64": (2, [0], 2000, 0, 0, 64, 30, 4, 16, 1, 33, 1900, 1990, 6, "bf16"),
+    "g16-64-20": (1, [0], 7400, 0, 0, 64, 30, 4, 16, 20, 33, 7300, 7380, 20, "bf16"),
+    "rank-0-20": (1, [0], 7400, 5, 0, 128, 30, 0, 32, 1, 33, 7300, 7380, 20, "bf16"),
+    "odd-rank": (1, [0], 4000, 10, 0, 128, 60, 13, 32, 2, 10, 3900, 3990, 10, "bf16"),
+    "many-epochs": (1, [66 * i for i in range(40)], 2700, 20, 0, 64, 8, 4, 16, 5, 70, 2600, 2600, 7, "bf16"),
+    "many-epochs-19": (1, [180 * i for i in range(40)], 7200, 20, 0, 64, 8, 4, 16, 5, 70, 7100, 7200, 19, "bf16"),
+    "early-rows": (1, [0], 7400, 0, 0, 128, 200, 16, 32, 1, 4, 7400, 0, 20, "bf16"),
+    "early-row": (1, [0], 7400, 0, 1, 128, 200, 16, 32, 1, 4, 7400, 100, 1, "bf16"),
+    "past-the-keys-few": (1, [0], 4000, 20, 0, 128, 32, 8, 32, 1, 0, 3900, 4020, 6, "bf16"),
     "long": (1, [0], 30_000, 100, 0, 64, 32, 8, 32, 1, 500, 20_000, 30_050, 3, "bf16"),
 }
-SHORT = {f"{k}-{m}": v[:13] + (min(m, v[13]), v[14]) for k, v in CASES.items() if v[14] == "bf16" and v[13] > 1
-         for m in (2, 45)}
+SHORT = {f"{k}-{m}": v[:13] + (m, v[14]) for k, v in CASES.items() if v[14] == "bf16" and v[13] > 2 for m in (1, 2)}
 
 
 @pytest.mark.parametrize("name", list(CASES) + list(FEW) + list(SHORT))
@@ -88,12 +95,12 @@ def test_window(name):
         if at is not None:  # about 25 above the other logits at d = 128
             q[:, i] += 2.0 * k[:, :, min(max(at, 0), n - 1)]
     q = s64.rounded(q, dtype)
-    few = not s64.rebuilt(dtype, n_q, r)
-    logits = p.logits(q, few)
-    if n_act:
-        logits = np.concatenate([logits, s64.exact_logits(q, ka)], 3)
-    ref, rlse, mag = s64.softmax(logits, visible, v)
-    tol = s64.tolerances(q, k, n, r, dtype, p.residuals() if few else None)
+    refs = []
+    for few in s64.forms(dtype):
+        logits = p.logits(q, few)
+        if n_act:
+            logits = np.concatenate([logits, s64.exact_logits(q, ka)], 3)
+        refs.append((*s64.softmax(logits, visible, v), s64.tolerances(q, k, n, r, dtype, p.residuals() if few else None)))
     dt = p.cfg.torch_dtype
     calibs, cache, qd = p.blocks(), p.on_device(), s64.dev(q, dt)
     kd, vd = (s64.dev(ka, dt), s64.dev(va, dt)) if n_act else (None, None)
@@ -105,7 +112,7 @@ def test_window(name):
         qw.quantwm_attend_window(p.cfg, calibs, p.starts, cache, n_pk, kd, vd, n_act, qd, n_q, q_start, frame, n_sink,
                                  window, out, lse, ws)
         torch.cuda.synchronize()
-        s64.check(out, lse, ref, rlse, mag, tol)
+        s64.check_any(out, lse, refs)
         only = torch.full_like(qd, 7.0)  # without the log-sum-exp
         qw.quantwm_attend_window(p.cfg, calibs, p.starts, cache, n_pk, kd, vd, n_act, qd, n_q, q_start, frame, n_sink,
                                  window, only, None, ws)
@@ -132,9 +139,9 @@ def _calibrated(cfg, gen, blocks=1):
 
 @pytest.mark.parametrize("d,r,dtype", [(64, 4, "bf16"), (128, 6, "bf16"), (128, 32, "bf16"), (64, 13, "f32")])
 def test_window_over_sparse_rows(d, r, dtype):
-    """Sparse and slot-addressed PSAC rows give the same bits through a window (with so
-    many Queries that one kernel serves both)."""
-    H, n, nq, starts = 3, 1200, 120 if dtype == "bf16" else 2100, [0, 90, 500, 800]
+    """Sparse and slot-addressed PSAC rows give the same results through a window: the
+    same bits where one kernel serves both, else (fp32) what the order of sums allows."""
+    H, n, nq, starts = 3, 1200, 120, [0, 90, 500, 800]
     gen = torch.Generator(device=DEV).manual_seed(d + r)
     got = []
     cfgs = [qw.make_config(1, H, d, 16, 32, r, 4, n, dtype, st, coef_stage=n) for st in (0, 4)]
@@ -152,11 +159,20 @@ def test_window_over_sparse_rows(d, r, dtype):
             out, lse = torch.full_like(q, 7.0), torch.empty((1, H, nq), device=DEV)
             qw.quantwm_attend_window(cfg, calibs, starts, cache, n, ka, va, 50, q, nq, n - 20, 10, 100, 400, out, lse, ws)
             got.append((out, lse))
+    # a logit errs by (d + r + 8) 2^-24 of its terms, at most |q| |khat| / sqrt(d) with Keys decoded
+    # to within their own size; a weight by that and n 2^-24, in O and in the sum; twice, for
+    # either side; |vhat| is at most twice the largest Value
+    size = lambda x: float(x.double().square().sum(3).max().sqrt())  # noqa: E731
+    dl = (d + r + 8) * 2.0 ** -24 * size(q) * 2 * max(size(k), size(ka)) / d ** 0.5 + n * 2.0 ** -24
     for i in range(2):
-        assert torch.equal(got[i][0], got[2 + i][0]) and torch.equal(got[i][1], got[2 + i][1]), i
+        if dtype == "bf16":
+            assert torch.equal(got[i][0], got[2 + i][0]) and torch.equal(got[i][1], got[2 + i][1]), i
+        else:
+            assert (got[i][0] - got[2 + i][0]).abs().max() <= 2 * (2 * dl + 2.0 ** -22) * 2 * float(max(v.abs().max(), va.abs().max()))
+            assert (got[i][1] - got[2 + i][1]).abs().max() <= 2 * (dl + 2.0 ** -22 * float(got[i][1].abs().max()))
 
 
-@pytest.mark.parametrize("nq", [40, 120])
+@pytest.mark.parametrize("nq", [1, 40, 120])
 @pytest.mark.parametrize("dtype,st", [("bf16", 0), ("bf16", 1), ("f32", 0)])
 def test_tiles_out_of_reach_are_not_read(dtype, st, nq):
     """Slots between the sinks' last tile and the window's first one, and past the
@@ -179,12 +195,13 @@ def test_tiles_out_of_reach_are_not_read(dtype, st, nq):
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
 
 
+@pytest.mark.parametrize("nq,step", [(60, 20), (1, 20), (1, 40)])
 @pytest.mark.parametrize("st", [0, 1])
-def test_neighbour_epochs_of_other_magnitude(st):
+def test_neighbour_epochs_of_other_magnitude(st, nq, step):
     """An epoch boundary inside a chunk, Values around 2^-100 on one side and steps near
-    the largest binary16 on the other, few Queries: neither side's keys reach the
-    other's Queries as an infinity or weight."""
-    H, d, kc, nq, starts, n = 2, 128, 16, 60, [0, 100, 200], 300
+    the largest binary16 on the other, one Query and several: neither side's keys reach
+    the other's Queries as an infinity or weight."""
+    H, d, kc, starts, n = 2, 128, 16, [0, 100, 200], 300
     scale = [2.0 ** -100, 2.0 ** 14, 2.0 ** -100]
     rng = np.random.default_rng(st)
     p = s64.Packed(rng, 1, H, d, kc, 32, 4, "bf16", st, [0], n)  # Keys and formats; Values and tables below
@@ -197,14 +214,15 @@ def test_neighbour_epochs_of_other_magnitude(st):
         oracle.append(p.ocfg, p.tables[e], p.cache, starts[e], k, v)
     q = s64.rounded(rng.standard_normal((1, nq, H, d)), "bf16")
     k, v = p.keys_values()
-    # 20 rows a frame: frame 0 sees epoch 0, frames 1 and 2 windows of one epoch each and its neighbours' last keys
-    hi = 100 + 20 * (np.arange(nq) // 20)
+    # frames see windows of 100 keys, of two epochs but for step 20's first
+    hi = 80 + step * (np.arange(nq) // step + 1)
     visible = (np.arange(n) < hi[:, None]) & (np.arange(n) >= hi[:, None] - 100)
-    ref, rlse, mag = s64.softmax(p.logits(q, True), visible, v)
+    refs = [(*s64.softmax(p.logits(q, few), visible, v), s64.tolerances(q, k, n, 4, "bf16", p.residuals() if few else None))
+            for few in (False, True)]
     qd = s64.dev(q, torch.bfloat16)
     out, lse = torch.full_like(qd, 7.0), torch.empty(1, H, nq, device=DEV)
-    qw.quantwm_attend_window(p.cfg, p.blocks(), starts, p.on_device(), n, None, None, 0, qd, nq, 80, 20, 0, 100, out, lse)
-    s64.check(out, lse, ref, rlse, mag, s64.tolerances(q, k, n, 4, "bf16", p.residuals()))
+    qw.quantwm_attend_window(p.cfg, p.blocks(), starts, p.on_device(), n, None, None, 0, qd, nq, 80, step, 0, 100, out, lse)
+    s64.check_any(out, lse, refs)
 
 
 def test_a_window_of_everything_is_attention_over_epochs():
