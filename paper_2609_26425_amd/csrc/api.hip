@@ -764,7 +764,7 @@ quantwm_status quantwm_attend_shared(const quantwm_config* prefix_cfg, const voi
     set_planes(f, a, qwm::attend_splits(a.n_q, f->heads, f->batch, n_keys, device_cus(), qwm::elem_bytes(*f)), at);
     return launch_attend(f, a, false, s);
   };
-  qwm::SharedArgs c{};
+  qwm::JoinArgs c{};
   c.n_q = n_q; c.heads = cfg->heads; c.batch = cfg->batch; c.out = out; c.lse = lse_out;
   if (p.prefix > 0) {
     qwm::AttendArgs a = attend_args(prefix_cfg, prefix_calibs, n_epochs, epoch_start, prefix_cache, n_prefix, nullptr,
@@ -780,8 +780,8 @@ quantwm_status quantwm_attend_shared(const quantwm_config* prefix_cfg, const voi
       return hip_fail(e, "attend launch (own keys)");
     c.own_o = a.part_o; c.own_ml = a.part_ml; c.n_own = a.n_split;
   }
-  if ((e = qwm::launch_shared_combine(c, cfg->head_dim, cfg->dtype == QWM_BF16, s)) != hipSuccess)
-    return hip_fail(e, "shared combine launch");
+  if ((e = qwm::launch_join(c, cfg->head_dim, cfg->dtype == QWM_BF16, s)) != hipSuccess)
+    return hip_fail(e, "join launch");
   return ok();
 }
 

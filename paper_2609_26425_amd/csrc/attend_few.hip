@@ -326,7 +326,8 @@ __global__ __launch_bounds__(64 * few_waves(NQ, TAB)) void attend_few_kernel(con
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int key = k0 + 16 * (i / 4) + 4 * kq + i % 4;
-          if (key >= min(khi, lim[n]) || key < klo || (key >= sinks && key < wfrom[n])) s[i / 4][n][i % 4] = -__builtin_inff();
+          const bool hide = (key >= min(khi, lim[n])) | (key < klo) | ((key >= sinks) & (key < wfrom[n]));
+          s[i / 4][n][i % 4] = hide ? -__builtin_inff() : s[i / 4][n][i % 4];
         }
     }
 #pragma unroll

@@ -128,34 +128,41 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_few_f32_kernel(const At
     }
   };
 
-  // ---- Query: step st of lane half hf is channel hf D/2 + st
-  float q[HK], ureg[RP > 0 ? RP / 2 : 1];
-  const float* qrow = reinterpret_cast<const float*>(a.q) + ((int64_t(b) * a.n_q + (qvalid ? qi : qa)) * a.heads + h) * D + hf * HK;
-#pragma unroll
-  for (int st = 0; st < HK; st += 4) {
-    const float4 v = *reinterpret_cast<const float4*>(qrow + st);
-    q[st] = qvalid ? v.x : 0.0f;
-    q[st + 1] = qvalid ? v.y : 0.0f;
-    q[st + 2] = qvalid ? v.z : 0.0f;
-    q[st + 3] = qvalid ? v.w : 0.0f;
-  }
+  // ---- everything that a part starts with, in flight at once: the packed fields, the
+  // Query (step st of lane half hf is channel hf D/2 + st) and U_r
   Regs P;
   if (!act && t0 < t1) load(P, t0 + wave < t1 ? t0 + wave : t1 - 1);
+  float q[HK], ureg[RP > 0 ? RP / 2 : 1];
+  float4 qv[HK / 4], uv[HK / 4];
+  const float* qrow = reinterpret_cast<const float*>(a.q) + ((int64_t(b) * a.n_q + (qvalid ? qi : qa)) * a.heads + h) * D + hf * HK;
+  const float* urow = reinterpret_cast<const float*>(slab + a.o_u_t) + int64_t(l32 < r ? l32 : 0) * D + hf * HK;
+#pragma unroll
+  for (int st = 0; st < HK / 4; ++st) qv[st] = reinterpret_cast<const float4*>(qrow)[st];
+  if (RP > 0 && !act) {
+#pragma unroll
+    for (int st = 0; st < HK / 4; ++st) uv[st] = reinterpret_cast<const float4*>(urow)[st];
+  }
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int st = 0; st < HK / 4; ++st) {
+    q[4 * st] = qvalid ? qv[st].x : 0.0f;
+    q[4 * st + 1] = qvalid ? qv[st].y : 0.0f;
+    q[4 * st + 2] = qvalid ? qv[st].z : 0.0f;
+    q[4 * st + 3] = qvalid ? qv[st].w : 0.0f;
+  }
   if constexpr (RP > 0) {
 #pragma unroll
     for (int i = 0; i < RP / 2; ++i) ureg[i] = 0.0f;
     if (!act) {  // q U_r (rows = ranks of U_r^T)
-      const float* urow = reinterpret_cast<const float*>(slab + a.o_u_t) + int64_t(l32 < r ? l32 : 0) * D + hf * HK;
       f32x16 u;
 #pragma unroll
       for (int i = 0; i < 16; ++i) u[i] = 0.0f;
 #pragma unroll
-      for (int st = 0; st < HK; st += 4) {
-        const float4 v = *reinterpret_cast<const float4*>(urow + st);
-        u = MF::run(l32 < r ? v.x : 0.0f, q[st], u);
-        u = MF::run(l32 < r ? v.y : 0.0f, q[st + 1], u);
-        u = MF::run(l32 < r ? v.z : 0.0f, q[st + 2], u);
-        u = MF::run(l32 < r ? v.w : 0.0f, q[st + 3], u);
+      for (int st = 0; st < HK / 4; ++st) {
+        u = MF::run(l32 < r ? uv[st].x : 0.0f, q[4 * st], u);
+        u = MF::run(l32 < r ? uv[st].y : 0.0f, q[4 * st + 1], u);
+        u = MF::run(l32 < r ? uv[st].z : 0.0f, q[4 * st + 2], u);
+        u = MF::run(l32 < r ? uv[st].w : 0.0f, q[4 * st + 3], u);
       }
 #pragma unroll
       for (int i = 0; i < RP / 2; ++i) ureg[i] = u[i];
@@ -183,7 +190,9 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_few_f32_kernel(const At
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int key = k0 + acc_row(i, hf);
-        if (key >= khi || key < klo || (key >= int(reach.ns) && key < wfrom)) s[i] = -__builtin_inff();
+        // a select: as a conditional store the compiler branched for each and copied all of s
+        const bool hide = (key >= khi) | (key < klo) | ((key >= int(reach.ns)) & (key < wfrom));
+        s[i] = hide ? -__builtin_inff() : s[i];
       }
     }
     float mt = -__builtin_inff();
@@ -221,10 +230,8 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_few_f32_kernel(const At
   };
 
   if (!act) {
-    auto decode = [&](const float* mu_row, uint32_t code, uint32_t zb, uint32_t sb, uint32_t sg, int grp_u, float (&x)[16],
+    auto decode = [&](const float (&mu)[16], uint32_t code, uint32_t zb, uint32_t sb, uint32_t sg, int grp_u, float (&x)[16],
                       bool in) __attribute__((always_inline)) {
-      float mu[16];
-      load_vals<float, 16>(mu_row, mu);
       const uint32_t z = (0x6400u + ((zb >> (2 * (grp_u % 4))) & 3)) * 0x00010001u;
       const _Float16 c = SI8 ? (_Float16)(int)sb : (_Float16)0;
       const float s = in ? (float)__builtin_bit_cast(_Float16, uint16_t(SI8 ? sg : sb)) : 0.0f;
@@ -235,21 +242,38 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_few_f32_kernel(const At
       const float* mk = gK + int64_t(int(P.k_id) < Kc ? int(P.k_id) : Kc - 1) * D;
       const float* mv = gV + int64_t(int(P.v_id) < Kc ? int(P.v_id) : Kc - 1) * D;
       const bool in = k0 + l32 >= g.lo;  // not a key of the neighbouring epoch before the segment's first
+      // both centroid rows are gathered before either is used (d = 64; the registers of
+      // d = 128 hold one side at a time)
+      constexpr bool BOTH = W == 2;
+      float muk[W][16], muv[W][16];
+      auto gather = [&](const float* row, float (&mu)[W][16]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < W; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4 v = reinterpret_cast<const float4*>(row + 16 * u)[i];
+            mu[u][4 * i] = v.x; mu[u][4 * i + 1] = v.y; mu[u][4 * i + 2] = v.z; mu[u][4 * i + 3] = v.w;
+          }
+      };
+      gather(mv, muv);
+      if constexpr (BOTH) gather(mk, muk);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int u = 0; u < W; ++u) {
         float x[16];
-        decode(mv + 16 * u, P.v_c[u], P.v_z[u], P.v_s[u], P.v_sg, grp[u], x, in);
+        decode(muv[u], P.v_c[u], P.v_z[u], P.v_s[u], P.v_sg, grp[u], x, in);
         float4* row = reinterpret_cast<float4*>(vt + l32 * FewTile<D>::ROW + hf * HK + 16 * u);
 #pragma unroll
         for (int i = 0; i < 4; ++i) row[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
       }
+      if constexpr (!BOTH) gather(mk, muk);
       f32x16 s;
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
       for (int u = 0; u < W; ++u) {
         float x[16];
-        decode(mk + 16 * u, P.k_c[u], P.k_z[u], P.k_s[u], P.k_sg, grp[u], x, true);
+        decode(muk[u], P.k_c[u], P.k_z[u], P.k_s[u], P.k_sg, grp[u], x, true);
 #pragma unroll
         for (int c = 0; c < 16; ++c) s = MF::run(x[c], q[16 * u + c], s);
       }

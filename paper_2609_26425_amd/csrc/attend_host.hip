@@ -58,61 +58,140 @@ __global__ __launch_bounds__(256) void attend_combine(const AttendArgs a) {
   if (a.lse && lane == 0) a.lse[bh * a.n_q + qi] = L > 0.0f ? M / sqrtf((float)D) + logf(L) : -__builtin_inff();
 }
 
-// attend_combine over two sets of planes: those of the shared prefix, whose rows
-// are the rollouts' rows one after the other, and those of the own keys. One wave
-// per output row, in the order of the output.
+// Log-sum-exp merge of partial planes for the windowed and shared-history forms: the
+// planes of the shared prefix, whose rows are the rollouts' rows one after the other,
+// and those of the own keys (the only ones of a windowed launch). Rows are taken in
+// the order of the output. Two forms, by what bounds them:
+//   - many planes of few rows: a wave per row, a lane per plane for the running maxima
+//     and sums, so that the merge waits for memory twice however many planes there are
+//     (25 planes of 480 rows: 8.7 us with a loop over the planes);
+//   - up to four planes of many rows: 16 lanes per row, so that a wave has four rows'
+//     loads in flight (bandwidth: 2 planes of 124,800 rows at d = 128).
+struct JoinRow {
+  int64_t at1, at2;  // the row in a plane of the prefix, of the own keys
+};
+__device__ inline JoinRow join_row(const JoinArgs& a, int64_t row) {
+  const uint32_t bi = uint32_t(row / a.heads), h = uint32_t(row % a.heads), b = bi / uint32_t(a.n_q), i = bi % uint32_t(a.n_q);
+  return {int64_t(h) * (a.batch * a.n_q) + bi, (int64_t(b) * a.heads + h) * a.n_q + i};
+}
+
 template <typename T, int D>
-__global__ __launch_bounds__(256) void shared_combine(const SharedArgs a) {
+__global__ __launch_bounds__(256) void join_planes(const JoinArgs a) {
   const int64_t row = int64_t(blockIdx.x) * 4 + threadIdx.x / 64, rows = int64_t(a.batch) * a.n_q * a.heads;
-  const int lane = threadIdx.x % 64;
+  const int lane = threadIdx.x % 64, n = a.n_prefix + a.n_own;
   if (row >= rows) return;
-  const int64_t bi = row / a.heads, b = bi / a.n_q, i = bi % a.n_q;  // bi: row of the prefix pass
-  const int h = int(row % a.heads);
-  const int64_t at1 = h * (a.batch * a.n_q) + bi, at2 = (b * a.heads + h) * a.n_q + i;
+  const JoinRow at = join_row(a, row);
   const float mscale = 1.4426950408889634f / sqrtf((float)D);
   constexpr int PL = D / 64;
   typedef float vecf __attribute__((ext_vector_type(PL)));
-  const float2* ml1 = reinterpret_cast<const float2*>(a.prefix_ml) + at1;
-  const float2* ml2 = reinterpret_cast<const float2*>(a.own_ml) + at2;
-  const float* o1 = a.prefix_o + at1 * D + lane * PL;
-  const float* o2 = a.own_o + at2 * D + lane * PL;
-  float M = -__builtin_inff();
-  for (int sp = 0; sp < a.n_prefix; ++sp) M = fmaxf(M, ml1[sp * rows].x);
-  for (int sp = 0; sp < a.n_own; ++sp) M = fmaxf(M, ml2[sp * rows].x);
+  auto ml_of = [&](int sp) {
+    return sp < a.n_prefix ? reinterpret_cast<const float2*>(a.prefix_ml)[sp * rows + at.at1]
+                           : reinterpret_cast<const float2*>(a.own_ml)[(sp - a.n_prefix) * rows + at.at2];
+  };
+  auto o_of = [&](int sp) {
+    const float* o = sp < a.n_prefix ? a.prefix_o + (sp * rows + at.at1) * D : a.own_o + ((sp - a.n_prefix) * rows + at.at2) * D;
+    return *reinterpret_cast<const vecf*>(o + lane * PL);
+  };
+  const float none = -__builtin_inff();
+  float M = none;
+  for (int s0 = 0; s0 < n; s0 += 64) M = fmaxf(M, s0 + lane < n ? ml_of(s0 + lane).x : none);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
   vecf o = {};
   float L = 0.0f;
-  auto add = [&](const float2 p, const vecf v) __attribute__((always_inline)) {
-    if (!(p.y > 0.0f)) return;  // no visible key of this row in that part
-    const float w = __builtin_amdgcn_exp2f((p.x - M) * mscale);
+  for (int s0 = 0; s0 < n; s0 += 64) {
+    const float2 p = s0 + lane < n ? ml_of(s0 + lane) : make_float2(none, 0.0f);
+    const float w = p.y > 0.0f ? __builtin_amdgcn_exp2f((p.x - M) * mscale) : 0.0f;  // 0: no visible key in that part
     L += w * p.y;
+    const int m = n - s0 < 64 ? n - s0 : 64;
+    for (int u0 = 0; u0 < m; u0 += 8) {
+      vecf v[8];
 #pragma unroll
-    for (int j = 0; j < PL; ++j) o[j] += w * v[j];
-  };
-#pragma unroll 4
-  for (int sp = 0; sp < a.n_prefix; ++sp) add(ml1[sp * rows], *reinterpret_cast<const vecf*>(o1 + sp * rows * D));
-#pragma unroll 4
-  for (int sp = 0; sp < a.n_own; ++sp) add(ml2[sp * rows], *reinterpret_cast<const vecf*>(o2 + sp * rows * D));
+      for (int u = 0; u < 8; ++u) v[u] = o_of(s0 + (u0 + u < m ? u0 + u : m - 1));
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        // (a part without a visible key leaves its O row unwritten)
+        const float wu = u0 + u < m ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), u0 + u)) : 0.0f;
+        if (wu > 0.0f) {
+#pragma unroll
+          for (int j = 0; j < PL; ++j) o[j] += wu * v[u][j];
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) L += __shfl_xor(L, s);
   const float inv = L > 0.0f ? 1.0f / L : 0.0f;
   T* orow = reinterpret_cast<T*>(a.out) + row * D + lane * PL;
 #pragma unroll
   for (int j = 0; j < PL; ++j) orow[j] = T(o[j] * inv);
-  if (a.lse && lane == 0) a.lse[at2] = L > 0.0f ? M / sqrtf((float)D) + logf(L) : -__builtin_inff();
+  if (a.lse && lane == 0) a.lse[at.at2] = L > 0.0f ? M / sqrtf((float)D) + logf(L) : none;
 }
 
-template <typename T>
-hipError_t launch_shared_combine_t(const SharedArgs& a, int d, hipStream_t s) {
-  const int64_t rows = int64_t(a.batch) * a.n_q * a.heads;
-  const dim3 grid((unsigned)((rows + 3) / 4));
-  if (d == 64) hipLaunchKernelGGL((shared_combine<T, 64>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((shared_combine<T, 128>), grid, dim3(256), 0, s, a);
-  return hipGetLastError();
+constexpr int kWidePlanes = 4;
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void join_rows(const JoinArgs a) {
+  const int64_t row = int64_t(blockIdx.x) * 16 + threadIdx.x / 16, rows = int64_t(a.batch) * a.n_q * a.heads;
+  const int l16 = threadIdx.x % 16, n = a.n_prefix + a.n_own;
+  if (row >= rows) return;
+  const JoinRow at = join_row(a, row);
+  const float mscale = 1.4426950408889634f / sqrtf((float)D);
+  constexpr int PL = D / 16;
+  typedef float vecf __attribute__((ext_vector_type(PL)));
+  float2 p[kWidePlanes];
+  vecf v[kWidePlanes];
+#pragma unroll
+  for (int sp = 0; sp < kWidePlanes; ++sp) {
+    p[sp] = make_float2(-__builtin_inff(), 0.0f);
+    if (sp < n) {
+      const bool pre = sp < a.n_prefix;
+      const int64_t r = pre ? sp * rows + at.at1 : (sp - a.n_prefix) * rows + at.at2;
+      p[sp] = reinterpret_cast<const float2*>(pre ? a.prefix_ml : a.own_ml)[r];
+      v[sp] = *reinterpret_cast<const vecf*>((pre ? a.prefix_o : a.own_o) + r * D + l16 * PL);
+    }
+  }
+  float M = -__builtin_inff(), L = 0.0f;
+#pragma unroll
+  for (int sp = 0; sp < kWidePlanes; ++sp) M = fmaxf(M, p[sp].x);
+  vecf o = {};
+#pragma unroll
+  for (int sp = 0; sp < kWidePlanes; ++sp) {
+    if (p[sp].y > 0.0f) {
+      const float w = __builtin_amdgcn_exp2f((p[sp].x - M) * mscale);
+      L += w * p[sp].y;
+#pragma unroll
+      for (int j = 0; j < PL; ++j) o[j] += w * v[sp][j];
+    }
+  }
+  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  typedef T vect __attribute__((ext_vector_type(PL)));
+  vect r;
+#pragma unroll
+  for (int j = 0; j < PL; ++j) r[j] = T(o[j] * inv);
+  *reinterpret_cast<vect*>(reinterpret_cast<T*>(a.out) + row * D + l16 * PL) = r;
+  if (a.lse && l16 == 0) a.lse[at.at2] = L > 0.0f ? M / sqrtf((float)D) + logf(L) : -__builtin_inff();
 }
 
 template <typename T, int D>
-hipError_t launch_combine(const AttendArgs& a, int batch, hipStream_t s) {
-  hipLaunchKernelGGL((attend_combine<T, D>), dim3((unsigned)((a.n_q + 3) / 4), (unsigned)a.heads, (unsigned)batch),
-                     dim3(256), 0, s, a);
+hipError_t launch_join_d(const JoinArgs& a, hipStream_t s) {
+  const int64_t rows = int64_t(a.batch) * a.n_q * a.heads;
+  // 16 lanes a row from four rows for every SIMD on
+  const bool wide = a.n_prefix + a.n_own <= kWidePlanes && rows >= 4096;
+  const int64_t wgs = (rows + (wide ? 15 : 3)) / (wide ? 16 : 4);
+  if (wgs > 0x7fffffff) return hipErrorInvalidValue;
+  if (wide) hipLaunchKernelGGL((join_rows<T, D>), dim3((unsigned)wgs), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((join_planes<T, D>), dim3((unsigned)wgs), dim3(256), 0, s, a);
   return hipGetLastError();
+}
+
+// The planes of one windowed launch.
+template <typename T, int D>
+hipError_t launch_join_own(const AttendArgs& a, int batch, hipStream_t s) {
+  JoinArgs j{};
+  j.own_o = a.part_o; j.own_ml = a.part_ml; j.n_own = a.n_split;
+  j.n_q = a.n_q; j.heads = a.heads; j.batch = batch; j.out = a.out; j.lse = a.lse;
+  return launch_join_d<T, D>(j, s);
 }
 
 template <typename T, int D>
@@ -123,7 +202,10 @@ hipError_t launch_d(const AttendArgs& a, int batch, bool logits, hipStream_t s) 
   else e = launch_attend_rp<T, D, 32>(a, batch, logits, s);
   // planes without an output: the caller joins them with others
   if (e != hipSuccess || logits || a.n_split == 1 || !a.out) return e;
-  return launch_combine<T, D>(a, batch, s);
+  if (a.windowed) return launch_join_own<T, D>(a, batch, s);
+  hipLaunchKernelGGL((attend_combine<T, D>), dim3((unsigned)((a.n_q + 3) / 4), (unsigned)a.heads, (unsigned)batch),
+                     dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 template <int D>
@@ -133,7 +215,7 @@ hipError_t launch_few_f32_d(const AttendArgs& a, int batch, hipStream_t s) {
   else if (a.rank <= 16) e = launch_attend_few_f32_rp<D, 16>(a, batch, s);
   else e = launch_attend_few_f32_rp<D, 32>(a, batch, s);
   if (e != hipSuccess || a.n_split == 1 || !a.out) return e;
-  return launch_combine<float, D>(a, batch, s);
+  return launch_join_own<float, D>(a, batch, s);
 }
 
 template <int D>
@@ -143,7 +225,7 @@ hipError_t launch_few_d(const AttendArgs& a, int batch, hipStream_t s) {
   else if (a.rank <= 16) e = launch_attend_few_rp<D, 16>(a, batch, s);
   else e = launch_attend_few_rp<D, 32>(a, batch, s);
   if (e != hipSuccess || a.n_split == 1 || !a.out) return e;
-  return launch_combine<bf16, D>(a, batch, s);
+  return launch_join_own<bf16, D>(a, batch, s);
 }
 
 // Parts that few_parts workgroups take for chunks_per_part = cpp: the most of any
@@ -229,8 +311,10 @@ hipError_t launch_attend_few(const AttendArgs& a, int d, int elem, int batch, hi
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_shared_combine(const SharedArgs& a, int d, bool bf16_out, hipStream_t s) {
-  return bf16_out ? launch_shared_combine_t<bf16>(a, d, s) : launch_shared_combine_t<float>(a, d, s);
+hipError_t launch_join(const JoinArgs& a, int d, bool bf16_out, hipStream_t s) {
+  if (d == 64) return bf16_out ? launch_join_d<bf16, 64>(a, s) : launch_join_d<float, 64>(a, s);
+  if (d == 128) return bf16_out ? launch_join_d<bf16, 128>(a, s) : launch_join_d<float, 128>(a, s);
+  return hipErrorInvalidValue;
 }
 
 size_t attend_lds_bytes(int d, int elem, int rank, int n_centroids, bool tables) {

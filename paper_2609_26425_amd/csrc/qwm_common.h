@@ -159,7 +159,7 @@ struct AttendArgs {
 // Joins the partial planes of attention over a shared prefix (one chunk of all
 // rollouts' rows: [n_prefix][H][batch * n_q]) with those over each rollout's own
 // keys ([n_own][batch * H][n_q]).
-struct SharedArgs {
+struct JoinArgs {
   const float *prefix_o, *prefix_ml, *own_o, *own_ml;
   int n_prefix, n_own;  // planes of each, 0 where there are no such keys
   int64_t n_q;
@@ -206,7 +206,7 @@ bool attend_few_takes(const quantwm_config& c, int64_t n_q, int64_t n_keys);
 int attend_few_planes(int64_t n_q, int heads, int batch, int64_t n_keys, int cus, int elem);
 bool attend_few_plan(AttendArgs& a, int batch, int cus, int elem, int most);
 hipError_t launch_attend_few(const AttendArgs& a, int d, int elem, int batch, hipStream_t s);
-hipError_t launch_shared_combine(const SharedArgs& a, int d, bool bf16_out, hipStream_t s);
+hipError_t launch_join(const JoinArgs& a, int d, bool bf16_out, hipStream_t s);
 hipError_t launch_rotary(const RotaryArgs& a, int d, bool bf16_data, bool halves, hipStream_t s);
 size_t attend_lds_bytes(int d, int elem, int rank, int n_centroids, bool tables_in_lds);
 constexpr int kMaxSplits = 16;

@@ -61,9 +61,70 @@ __device__ inline uint4 pack(const Vec16<T>& v) {
 template <typename T, int D, bool HALVES, int TT>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(const RotaryArgs a) {
   constexpr int P = D / 2, N = Vec16<T>::N, UNIT = HALVES ? 2 * N : N, UNITS = D / UNIT;
+  constexpr int VN = HALVES ? 2 : 1;  // vectors of a unit
   __shared__ __attribute__((aligned(16))) float2 cs[TT * P];
   const int64_t tok0 = int64_t(blockIdx.x) * TT;
   const int tokens = int(a.tokens - tok0 < TT ? a.tokens - tok0 : TT);
+  const int row = a.heads * UNITS, total = tokens * row;
+  const int64_t out_stride = int64_t(a.heads) * D;
+  struct Unit {
+    int64_t src, dst;  // first element of its first vector
+    int second, pair;  // distance of its second vector; its first pair's angle
+  };
+  auto unit_of = [&](int i) __attribute__((always_inline)) {
+    const int t = i / row, u = i % row, h = u / UNITS, c = u % UNITS;
+    int first, second = 0, pair;
+    if constexpr (HALVES) {
+      const int turned = a.pairs / N;  // units of the turned channels
+      pair = c * N;
+      first = c < turned ? c * N : 2 * a.pairs + (c - turned) * 2 * N;
+      second = c < turned ? a.pairs : N;
+    } else {
+      pair = c * (N / 2);
+      first = c * N;
+    }
+    return Unit{(tok0 + t) * a.token_stride + h * D + first, (tok0 + t) * out_stride + h * D + first, second, t * P + pair};
+  };
+  auto fetch = [&](const void* base, const Unit& u, uint4 (&to)[VN]) __attribute__((always_inline)) {
+    const T* in = static_cast<const T*>(base) + u.src;
+    to[0] = *reinterpret_cast<const uint4*>(in);
+    if constexpr (HALVES) to[1] = *reinterpret_cast<const uint4*>(in + u.second);
+  };
+  auto turn = [&](void* base, const Unit& un, const uint4 (&from)[VN]) __attribute__((always_inline)) {
+    T* out = static_cast<T*>(base) + un.dst;
+    const float2* c = cs + un.pair;
+    Vec16<T> u = unpack<T>(from[0]);
+    if constexpr (HALVES) {
+      Vec16<T> v = unpack<T>(from[1]);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float2 t = c[j];
+        const float x = u.x[j], y = v.x[j];
+        u.x[j] = __builtin_fmaf(x, t.x, -y * t.y);
+        v.x[j] = __builtin_fmaf(x, t.y, y * t.x);
+      }
+      *reinterpret_cast<uint4*>(out + un.second) = pack<T>(v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) {
+        const float2 t = c[j];
+        const float x = u.x[2 * j], y = u.x[2 * j + 1];
+        u.x[2 * j] = __builtin_fmaf(x, t.x, -y * t.y);
+        u.x[2 * j + 1] = __builtin_fmaf(x, t.y, y * t.x);
+      }
+    }
+    *reinterpret_cast<uint4*>(out) = pack<T>(u);
+  };
+  // the first units are on their way while the angles are computed
+  const int i0 = threadIdx.x;
+  Unit u0{};
+  uint4 q0[VN], k0[VN];
+  if (i0 < total) {
+    u0 = unit_of(i0);
+    fetch(a.q, u0, q0);
+    if (a.k) fetch(a.k, u0, k0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
   for (int i = threadIdx.x; i < tokens * P; i += kRotThreads) {
     const int p = i % P;
     const int64_t tok = tok0 + i / P;
@@ -86,49 +147,17 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(const RotaryArgs a)
     cs[i] = v;
   }
   __syncthreads();
-
-  const int row = a.heads * UNITS, total = tokens * row;
-  const int64_t out_stride = int64_t(a.heads) * D;
-  auto turn = [&](const T* in, T* out, const float2* c, int first, int second) __attribute__((always_inline)) {
-    if constexpr (HALVES) {
-      Vec16<T> u = unpack<T>(*reinterpret_cast<const uint4*>(in + first));
-      Vec16<T> v = unpack<T>(*reinterpret_cast<const uint4*>(in + second));
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float2 t = c[j];
-        const float x = u.x[j], y = v.x[j];
-        u.x[j] = __builtin_fmaf(x, t.x, -y * t.y);
-        v.x[j] = __builtin_fmaf(x, t.y, y * t.x);
-      }
-      *reinterpret_cast<uint4*>(out + first) = pack<T>(u);
-      *reinterpret_cast<uint4*>(out + second) = pack<T>(v);
-    } else {
-      Vec16<T> u = unpack<T>(*reinterpret_cast<const uint4*>(in + first));
-#pragma unroll
-      for (int j = 0; j < N / 2; ++j) {
-        const float2 t = c[j];
-        const float x = u.x[2 * j], y = u.x[2 * j + 1];
-        u.x[2 * j] = __builtin_fmaf(x, t.x, -y * t.y);
-        u.x[2 * j + 1] = __builtin_fmaf(x, t.y, y * t.x);
-      }
-      *reinterpret_cast<uint4*>(out + first) = pack<T>(u);
-    }
-  };
-  for (int i = threadIdx.x; i < total; i += kRotThreads) {
-    const int t = i / row, u = i % row, h = u / UNITS, c = u % UNITS;
-    int first, second = 0, pair;
-    if constexpr (HALVES) {
-      const int turned = a.pairs / N;  // units of the turned channels
-      pair = c * N;
-      first = c < turned ? c * N : 2 * a.pairs + (c - turned) * 2 * N;
-      second = c < turned ? first + a.pairs : first + N;
-    } else {
-      pair = c * (N / 2);
-      first = c * N;
-    }
-    const int64_t src = (tok0 + t) * a.token_stride + h * D, dst = (tok0 + t) * out_stride + h * D;
-    turn(static_cast<const T*>(a.q) + src, static_cast<T*>(a.q_out) + dst, cs + t * P + pair, first, second);
-    if (a.k) turn(static_cast<const T*>(a.k) + src, static_cast<T*>(a.k_out) + dst, cs + t * P + pair, first, second);
+  if (i0 < total) {
+    turn(a.q_out, u0, q0);
+    if (a.k) turn(a.k_out, u0, k0);
+  }
+  for (int i = i0 + kRotThreads; i < total; i += kRotThreads) {
+    const Unit u = unit_of(i);
+    uint4 qv[VN], kv[VN];
+    fetch(a.q, u, qv);
+    if (a.k) fetch(a.k, u, kv);
+    turn(a.q_out, u, qv);
+    if (a.k) turn(a.k_out, u, kv);
   }
 }
 

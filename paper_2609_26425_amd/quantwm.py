@@ -274,7 +274,7 @@ def _device():
     global _gpu
     if _gpu is None:
         _gpu = torch.cuda.is_available()
-    return torch.cuda.current_device() if _gpu else None
+    return torch._C._cuda_getDevice() if _gpu else None
 
 
 def _address(name, t, dtype, least, dev):
