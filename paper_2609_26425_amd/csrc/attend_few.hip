@@ -38,14 +38,17 @@ constexpr int few_waves(int nq, bool tab) { return !tab ? 4 : (nq == 1 ? 12 : 8)
 
 // LDS: the products q . mu of every centroid and Query ([256][16 NQ] floats: an id is a
 // byte, so none reads past it), the Value table (TAB, binary16) and a V^T tile per
-// wave, in 32-bit words (key pairs): 64 channels, 16 of each quarter, of 16 pairs + 4
-// words of padding, each quarter 16 words further. The pair stores of a wave (runs of 16
-// pairs in four quarters) and the 8-byte operand reads (16 rows, two key runs at a
-// time) are then free of bank conflicts.
+// wave, in 32-bit words (key pairs): 64 channels, 16 of each quarter, of 16 pairs + 2
+// words of padding, each quarter 8 words further. With 32 banks, the pair stores of 32
+// lanes (8 pairs in four quarters) and the 8-byte operand reads of 16 lanes (as many rows)
+// are then free of conflicts. The four lanes of a pair read their 16-byte pieces of one
+// table row together, at a quarter row's distance: at d = 128 the pieces of the upper
+// half are turned by two, so that these four too lie in banks of their own.
 template <int D, int NQ>
 struct FewLds {
-  static constexpr int SMU = 256 * 16 * NQ, ROW = 20, VW = 64 * ROW + 48, TS = D + 8;
-  static __device__ inline int at(int quarter) { return quarter * (16 * ROW + 16); }  // its first row
+  static constexpr int SMU = 256 * 16 * NQ, ROW = 18, QUARTER = 16 * ROW + 8, VW = 3 * QUARTER + 16 * ROW, TS = D + 8;
+  static __device__ inline int at(int quarter) { return quarter * QUARTER; }  // its first row
+  static __device__ inline int piece(int c) { return D == 128 ? (c & 8) | ((c + (c >> 3) * 2) & 7) : c; }
 };
 
 // Packed fields of one 32-key chunk in a lane between their load and their use: a quarter
@@ -214,7 +217,7 @@ __global__ __launch_bounds__(64 * few_waves(NQ, TAB)) void attend_few_kernel(con
       const uint4* sv = reinterpret_cast<const uint4*>(gV);
 #pragma unroll 1
       for (int i = threadIdx.x; i < Kc * PER_ROW; i += 64 * NW)
-        *reinterpret_cast<uint4*>(tabV + i / PER_ROW * LY::TS + i % PER_ROW * 8) = sv[i];
+        *reinterpret_cast<uint4*>(tabV + i / PER_ROW * LY::TS + LY::piece(i % PER_ROW) * 8) = sv[i];
     }
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -451,8 +454,10 @@ __global__ __launch_bounds__(64 * few_waves(NQ, TAB)) void attend_few_kernel(con
     auto values = [&](int u) __attribute__((always_inline)) {
       float m0[16], m1[16], x0[16], x1[16];
       const int c0 = vq * HV + 16 * u;
-      load_tab<true, bf16, 16>((TAB ? tabV + id0 * LY::TS : gV + id0 * D) + c0, m0);
-      load_tab<true, bf16, 16>((TAB ? tabV + id1 * LY::TS : gV + id1 * D) + c0, m1);
+      // (a word's two pieces stay neighbours)
+      const int at = TAB ? LY::piece(c0 / 8) * 8 : c0;
+      load_tab<true, bf16, 16>((TAB ? tabV + id0 * LY::TS : gV + id0 * D) + at, m0);
+      load_tab<true, bf16, 16>((TAB ? tabV + id1 * LY::TS : gV + id1 * D) + at, m1);
       const _Float16 y0 = scale_of(p.v_s[0], u), y1 = scale_of(p.v_s[1], u);
       const f16x2 cm0 = {y0, y0}, cm1 = {y1, y1};
       float s0 = SI8 ? (float)__builtin_bit_cast(_Float16, uint16_t(p.v_sg[0])) : (float)y0;
