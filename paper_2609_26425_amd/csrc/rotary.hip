@@ -57,7 +57,8 @@ __device__ inline uint4 pack(const Vec16<T>& v) {
 
 // TT tokens per workgroup. HALVES: pair p is channels (p, p + pairs), so a thread
 // holds a vector of each half; otherwise it is channels (2 p, 2 p + 1) of one vector.
-// Channels past the turned pairs (p >= pairs) are copied, through cos 1 and sin 0.
+// Channels past the turned pairs (p >= pairs) are copied (a product with cos 1 and sin 0
+// would lose the sign of a zero, and take a pair's second infinity into its first).
 template <typename T, int D, bool HALVES, int TT>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(const RotaryArgs a) {
   constexpr int P = D / 2, N = Vec16<T>::N, UNIT = HALVES ? 2 * N : N, UNITS = D / UNIT;
@@ -70,6 +71,7 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(const RotaryArgs a)
   struct Unit {
     int64_t src, dst;  // first element of its first vector
     int second, pair;  // distance of its second vector; its first pair's angle
+    int left;          // turned pairs from its first on
   };
   auto unit_of = [&](int i) __attribute__((always_inline)) {
     const int t = i / row, u = i % row, h = u / UNITS, c = u % UNITS;
@@ -83,7 +85,8 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(const RotaryArgs a)
       pair = c * (N / 2);
       first = c * N;
     }
-    return Unit{(tok0 + t) * a.token_stride + h * D + first, (tok0 + t) * out_stride + h * D + first, second, t * P + pair};
+    return Unit{(tok0 + t) * a.token_stride + h * D + first, (tok0 + t) * out_stride + h * D + first, second, t * P + pair,
+                a.pairs - pair};
   };
   auto fetch = [&](const void* base, const Unit& u, uint4 (&to)[VN]) __attribute__((always_inline)) {
     const T* in = static_cast<const T*>(base) + u.src;
@@ -100,8 +103,8 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(const RotaryArgs a)
       for (int j = 0; j < N; ++j) {
         const float2 t = c[j];
         const float x = u.x[j], y = v.x[j];
-        u.x[j] = __builtin_fmaf(x, t.x, -y * t.y);
-        v.x[j] = __builtin_fmaf(x, t.y, y * t.x);
+        u.x[j] = un.left > 0 ? __builtin_fmaf(x, t.x, -y * t.y) : x;
+        v.x[j] = un.left > 0 ? __builtin_fmaf(x, t.y, y * t.x) : y;
       }
       *reinterpret_cast<uint4*>(out + un.second) = pack<T>(v);
     } else {
@@ -109,8 +112,8 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(const RotaryArgs a)
       for (int j = 0; j < N / 2; ++j) {
         const float2 t = c[j];
         const float x = u.x[2 * j], y = u.x[2 * j + 1];
-        u.x[2 * j] = __builtin_fmaf(x, t.x, -y * t.y);
-        u.x[2 * j + 1] = __builtin_fmaf(x, t.y, y * t.x);
+        u.x[2 * j] = j < un.left ? __builtin_fmaf(x, t.x, -y * t.y) : x;
+        u.x[2 * j + 1] = j < un.left ? __builtin_fmaf(x, t.y, y * t.x) : y;
       }
     }
     *reinterpret_cast<uint4*>(out) = pack<T>(u);

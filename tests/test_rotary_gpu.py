@@ -137,3 +137,21 @@ def test_given_frequencies():
             u, v = want[:, t, :, 0::2].clone(), want[:, t, :, 1::2].clone()
             want[:, t, :, 0::2], want[:, t, :, 1::2] = -v, u
     assert (out - want).abs().max() <= 2.0 ** -21 * x.abs().max()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("halves,dims", [(False, (2, 2, 6)), (False, (44, 42, 40)), (True, (12, 2, 18)), (False, (0, 0, 0))])
+def test_channels_past_the_axes_are_copied(halves, dims, dtype):
+    """bit for bit: the sign of a zero, and an infinity beside a finite channel."""
+    cfg = qw.make_config(1, 3, 128, 16, 16, 0, 1, 1, dtype)
+    axes = qw.rotary_axes(cfg, dims, *GRID, pairs=qw.ROTARY_HALVES if halves else qw.ROTARY_ADJACENT)
+    x = torch.randn(1, 9, 3, 128, generator=torch.Generator().manual_seed(3)).to(cfg.torch_dtype)
+    part = x[..., sum(dims):]
+    part[..., 0], part[..., 1] = 1.5, -0.0
+    part[:, ::2, :, 0], part[:, ::3, :, 1] = -0.0, float("inf")
+    x = x.to(DEV)
+    out = torch.full_like(x, 7.0)
+    qw.quantwm_rotary(cfg, axes, x, None, 9, out, pos0=1000)
+    bits = torch.int16 if dtype == "bf16" else torch.int32
+    assert torch.equal(out[..., sum(dims):].view(bits), x[..., sum(dims):].view(bits))
+    assert out[..., : sum(dims)].isfinite().all()
