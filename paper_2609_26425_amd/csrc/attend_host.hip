@@ -272,7 +272,8 @@ bool attend_few_takes(const quantwm_config& c, int64_t n_q, int64_t n_keys) {
   // 256 rows decode less (d = 64, us here / tiled: 2 heads x 257 Queries x 362 keys 18 / 29; 8 x
   // 512 x 3,000 59 / 61; 8 x 1,024 x 3,000 95 / 89. d = 128: 2 x 257 x 362 27 / 48, 2 x 1,024 x
   // 3,000 82 / 92, 8 x 1,024 x 1,024 94 / 78).
-  const double units = double((n_q + kFewQ - 1) / kFewQ) * c.heads * c.batch * double((n_keys + kFewChunk - 1) / kFewChunk);
+  // (a launch without keys still has its blocks, a grid dimension)
+  const double units = double((n_q + kFewQ - 1) / kFewQ) * c.heads * c.batch * double(n_keys / kFewChunk + 1);
   return n_q <= 4096 && units <= (c.head_dim == 64 ? 16384 : 6144);
 }
 

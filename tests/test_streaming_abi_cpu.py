@@ -196,3 +196,12 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
     for bad in (dict(prefix_calibs=pcalib[:-1]), dict(prefix_cache=pcache[:-1]), dict(calib=calib[:-1]), dict(q=x[:1])):
         with pytest.raises(ValueError):
             qw.quantwm_attend_shared(**{**good, **bad})
+
+
+def test_window_without_keys_over_many_blocks():
+    """512 rollouts of 4,096 fp32 Queries are more blocks of 32 than a grid dimension has,
+    whether they see keys or not: they take blocks of 256, unsplit."""
+    lib = qw.library()
+    cfg = _cfg(batch=512, dtype="f32")
+    for n_cache in (0, 64):
+        assert lib.quantwm_attend_window_workspace_bytes(ctypes.byref(cfg), n_cache, 0, 4096, 1, 0, 16) == 0
