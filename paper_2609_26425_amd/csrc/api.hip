@@ -789,6 +789,8 @@ quantwm_status quantwm_rotary_init(const quantwm_config* cfg, const int32_t* dim
                                    double base, int32_t pairs, quantwm_rotary_axes* out) {
   QWM_TRY(check_cfg(cfg));
   if (!dims || !out) return fail(QWM_ERR_INVALID_ARG, "dims or out is null");
+  if (pairs != QWM_ROTARY_ADJACENT && pairs != QWM_ROTARY_HALVES)
+    return fail(QWM_ERR_INVALID_ARG, "pairs must be QWM_ROTARY_ADJACENT or QWM_ROTARY_HALVES");
   if (!(base > 0.0) || !std::isfinite(base)) return fail(QWM_ERR_INVALID_ARG, "base must be finite and > 0");
   quantwm_rotary_axes a{};
   a.pairs = pairs;
@@ -825,8 +827,8 @@ quantwm_status quantwm_rotary(const quantwm_config* cfg, const quantwm_rotary_ax
   if (sum > cfg->head_dim) return fail(QWM_ERR_INVALID_ARG, "dims sum to more than head_dim");
   if (axes->pairs == QWM_ROTARY_HALVES && sum % 16)
     return fail(QWM_ERR_UNSUPPORTED, "with QWM_ROTARY_HALVES dims must sum to a multiple of 16");
-  for (int p = 0; p < sum / 2; ++p)
-    if (!std::isfinite(axes->freq[p])) return fail(QWM_ERR_INVALID_ARG, "freq[%d] is not finite", p);
+  for (int p = 0; p < sum / 2; ++p)  // nor may an angle overflow
+    if (!std::isfinite(axes->freq[p] * 2147483648.0)) return fail(QWM_ERR_INVALID_ARG, "freq[%d] is not finite or too large", p);
   if (n == 0) return ok();
   QWM_TRY(check_dev(q, "q"));
   QWM_TRY(check_dev(q_out, "q_out"));
@@ -837,6 +839,8 @@ quantwm_status quantwm_rotary(const quantwm_config* cfg, const quantwm_rotary_ax
   if (token_stride < row || token_stride * elem % 16 || token_stride > (int64_t(1) << 40))
     return fail(QWM_ERR_INVALID_ARG, "token_stride must be at least heads * head_dim and a multiple of 16 bytes");
   if (n > kMaxPositions / cfg->batch) return fail(QWM_ERR_UNSUPPORTED, "more than %lld tokens", (long long)kMaxPositions);
+  if (token_stride > (int64_t(1) << 59) / (n * cfg->batch))
+    return fail(QWM_ERR_INVALID_ARG, "token_stride reaches past any memory");
   if (pos) {
     if (reinterpret_cast<uintptr_t>(pos) & 3) return fail(QWM_ERR_INVALID_ARG, "pos is not 4-byte aligned");
   } else {

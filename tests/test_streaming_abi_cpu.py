@@ -161,6 +161,8 @@ def test_rotary_axes():
     for dims in ((3, 2, 2), (64, 64, 2), (-2, 4, 4)):
         with pytest.raises(qw.QuantwmError):
             qw.rotary_axes(cfg, dims, 4, 5)
+    with pytest.raises(qw.QuantwmError, match="pairs"):
+        qw.rotary_axes(cfg, (44, 42, 42), 4, 5, pairs=2)
     for base in (0.0, -1.0, float("inf"), float("nan")):
         with pytest.raises(qw.QuantwmError):
             qw.rotary_axes(cfg, (44, 42, 42), 4, 5, base=base)
@@ -205,3 +207,12 @@ def test_window_without_keys_over_many_blocks():
     cfg = _cfg(batch=512, dtype="f32")
     for n_cache in (0, 64):
         assert lib.quantwm_attend_window_workspace_bytes(ctypes.byref(cfg), n_cache, 0, 4096, 1, 0, 16) == 0
+
+
+@pytest.mark.parametrize("kw,word", [
+    # an angle past the doubles, for positions below 2^31; a stride whose bytes pass 64 bits
+    (dict(axes=_axes(freq=1e300)), "freq"), (dict(n=0x7fff0000, stride=1 << 40), "stride"),
+])
+def test_rotary_refuses_what_overflows(kw, word):
+    assert _rotary(**kw) == qw.ERR_INVALID_ARG
+    assert word in qw.quantwm_last_error()
