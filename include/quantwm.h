@@ -322,9 +322,11 @@ size_t quantwm_attend_epochs_workspace_bytes(const quantwm_config* cfg, int32_t 
  * token-causal window (the Query's own position and the window - 1 before it); a
  * window of W F positions shows the Query's frame and the W - 1 before it; a
  * window of every position is quantwm_attend_epochs. A Query that sees no key
- * has O = 0 and lse = -inf. Only the tiles of 64 keys that hold a visible key of a
- * block of 256 Queries are read, so time and bytes go by n_sink + window, not by
- * n_cache. n_epochs >= 1 (1: one calibration block, epoch_start may be NULL);
+ * has O = 0 and lse = -inf. Only tiles of at most 64 keys that hold a visible key of a
+ * block of at most 256 Queries are read, so time and bytes go by n_sink + window, not by
+ * n_cache. Few Queries take Keys as they are packed (centroid and residual) instead of
+ * rounded to the table type, so results differ by such roundings between launches of
+ * few and of many Queries. n_epochs >= 1 (1: one calibration block, epoch_start may be NULL);
  * n_act may be 0; n_sink and window are >= 0. Everything else as for
  * quantwm_attend_epochs, the optional workspace included. */
 quantwm_status quantwm_attend_window(const quantwm_config* cfg, const void* calibs, int32_t n_epochs,
@@ -334,8 +336,8 @@ quantwm_status quantwm_attend_window(const quantwm_config* cfg, const void* cali
                                      int64_t window, void* out, float* lse_out, void* workspace,
                                      size_t workspace_bytes, void* stream);
 
-/* Workspace bytes of quantwm_attend_window's key split (0 where the launch does
- * not split, or the arguments are invalid). */
+/* Workspace bytes of quantwm_attend_window's key split: enough for any q_start and
+ * epochs (0 where no such launch splits, or the arguments are invalid). */
 size_t quantwm_attend_window_workspace_bytes(const quantwm_config* cfg, int64_t n_cache, int64_t n_act, int64_t n_q,
                                              int32_t frame_tokens, int64_t n_sink, int64_t window);
 

