@@ -81,9 +81,10 @@ __global__ __launch_bounds__(64 * few_waves(NQ, TAB)) void attend_few_kernel(con
   const int Kc = a.n_centroids, r = a.rank;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l16 = lane % 16,
             kq = lane / 16;
-  const int part = int(blockIdx.x), h = int(blockIdx.y), b = int(blockIdx.z / uint32_t(a.q_blocks));
-  const int64_t bh = int64_t(b) * a.heads + h, n_bh = int64_t(a.heads) * (gridDim.z / uint32_t(a.q_blocks));
-  const int qa = int(blockIdx.z % uint32_t(a.q_blocks)) * a.block_rows, rows = min(a.block_rows, int(a.n_q) - qa);
+  const FewPlace place = few_place(a, blockIdx.x, gridDim.x);
+  const int part = place.part, h = place.h, b = place.b;
+  const int64_t bh = place.bh, n_bh = place.n_bh;
+  const int qa = place.block * a.block_rows, rows = min(a.block_rows, int(a.n_q) - qa);
   const int64_t nc = a.n_cache + a.n_act;
   const uint32_t F = uint32_t(a.frame_tokens);
   const FewReach reach = few_reach(a.q_start, F, nc, a.n_sink, a.window, a.windowed != 0, uint32_t(qa), uint32_t(qa + rows));
@@ -608,7 +609,7 @@ hipError_t launch_k(const AttendArgs& a, int batch, hipStream_t s) {
     if (e != hipSuccess) return e;
     raised.fetch_or(bit, std::memory_order_release);
   }
-  const dim3 grid((unsigned)a.n_split, (unsigned)a.heads, (unsigned)(a.q_blocks * batch));
+  const dim3 grid((unsigned)a.n_split * (unsigned)a.heads * (unsigned)(a.q_blocks * batch));
   hipLaunchKernelGGL((attend_few_kernel<D, G, RP, NQ, TAB, SI8>), grid, dim3(64 * few_waves(NQ, TAB)), lds, s, a);
   return hipGetLastError();
 }

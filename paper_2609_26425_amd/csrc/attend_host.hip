@@ -263,6 +263,8 @@ int64_t few_want(int64_t n_q, int heads, int batch, int64_t chunks, int cus, int
 
 bool attend_few_takes(const quantwm_config& c, int64_t n_q, int64_t n_keys) {
   if (c.storage & QWM_STORE_SPARSE) return false;
+  // (one grid dimension holds all parts: at most 65 of 768 threads for each head)
+  if (int64_t(c.heads) * c.batch > 65536) return false;
   // BF16: one block of rows, with coefficient rows of whole words, over enough keys that
   // decoding them outweighs the merge of the waves' O rows (d = 128, 12 heads, us here /
   // tiled: 1 Query x 300 keys 13 / 15, x 30,000 33 / 55; 16 x 1,000 20 / 18, x 8,000 27 / 28, x

@@ -4,6 +4,7 @@
 #pragma once
 
 #include "qwm_common.h"
+#include "xcd_order.h"
 
 namespace qwm {
 
@@ -58,6 +59,41 @@ inline __host__ __device__ FewSegment few_segment_of(const AttendArgs& a, int i,
 }
 
 #ifdef __HIPCC__
+// What workgroup L of n runs, in a launch of n_split parts of every unit (a Query block of
+// a head). Two orders:
+//   - few units, whose key range is cut: the parts of a unit on one XCD, so that its tables
+//     come from one L2 (40 heads x 1 Query x 30,000 keys: 52.8 us, with the parts dealt
+//     round the XCDs 53.9);
+//   - units enough for every CU, so that a part is a whole segment: part by part, the
+//     first segments of all units before the second. The exact chunk's parts, often a few
+//     keys, then fill in behind the packed ones instead of standing between them (16
+//     rollouts x 30 heads, 130 packed keys and one exact: 30 -> 21 us).
+struct FewPlace {
+  int part, h, b, block;
+  int64_t bh, n_bh;
+};
+__device__ inline FewPlace few_place(const AttendArgs& a, uint32_t L, uint32_t n) {
+  const uint32_t parts = uint32_t(a.n_split), units = n / parts, heads = uint32_t(a.heads);
+  uint32_t part, u;
+  if (units >= 256) {
+    part = L / units;
+    u = L % units;
+  } else {
+    const uint32_t t = qwm_xcd_task(L, n);
+    u = t / parts;
+    part = t % parts;
+  }
+  const uint32_t bb = u / heads, blocks = uint32_t(a.q_blocks);
+  FewPlace p;
+  p.part = int(part);
+  p.h = int(u % heads);
+  p.b = int(bb / blocks);
+  p.block = int(bb % blocks);
+  p.bh = int64_t(p.b) * heads + uint32_t(p.h);
+  p.n_bh = units / blocks;
+  return p;
+}
+
 // The segment of part `part`, and the parts before it: a lane counts for each epoch.
 __device__ inline int few_segment_at(const AttendArgs& a, const FewReach& r, int part, int lane, int& before) {
   static_assert(kMaxEpochs == 64, "a lane per epoch");

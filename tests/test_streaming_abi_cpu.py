@@ -207,6 +207,9 @@ def test_window_without_keys_over_many_blocks():
     cfg = _cfg(batch=512, dtype="f32")
     for n_cache in (0, 64):
         assert lib.quantwm_attend_window_workspace_bytes(ctypes.byref(cfg), n_cache, 0, 4096, 1, 0, 16) == 0
+    # nor are more heads taken than one dimension has room for, in parts
+    many = _cfg(batch=40_000)
+    assert lib.quantwm_attend_window_workspace_bytes(ctypes.byref(many), 64, 0, 1, 1, 0, 16) == 0
 
 
 @pytest.mark.parametrize("kw,word", [
