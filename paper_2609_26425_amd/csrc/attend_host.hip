@@ -70,14 +70,16 @@ __global__ __launch_bounds__(256) void attend_combine(const AttendArgs a) {
 struct JoinRow {
   int64_t at1, at2;  // the row in a plane of the prefix, of the own keys
 };
-__device__ inline JoinRow join_row(const JoinArgs& a, int64_t row) {
-  const uint32_t bi = uint32_t(row / a.heads), h = uint32_t(row % a.heads), b = bi / uint32_t(a.n_q), i = bi % uint32_t(a.n_q);
+// (32-bit quotients: a 64-bit one is some 150 instructions)
+__device__ inline JoinRow join_row(const JoinArgs& a, uint32_t row) {
+  const uint32_t bi = row / uint32_t(a.heads), h = row % uint32_t(a.heads), b = bi / uint32_t(a.n_q), i = bi % uint32_t(a.n_q);
   return {int64_t(h) * (a.batch * a.n_q) + bi, (int64_t(b) * a.heads + h) * a.n_q + i};
 }
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void join_planes(const JoinArgs a) {
-  const int64_t row = int64_t(blockIdx.x) * 4 + threadIdx.x / 64, rows = int64_t(a.batch) * a.n_q * a.heads;
+  const int64_t rows = int64_t(a.batch) * a.n_q * a.heads;
+  const uint32_t row = blockIdx.x * 4 + threadIdx.x / 64;
   const int lane = threadIdx.x % 64, n = a.n_prefix + a.n_own;
   if (row >= rows) return;
   const JoinRow at = join_row(a, row);
@@ -93,21 +95,27 @@ __global__ __launch_bounds__(256) void join_planes(const JoinArgs a) {
     return *reinterpret_cast<const vecf*>(o + lane * PL);
   };
   const float none = -__builtin_inff();
-  float M = none;
-  for (int s0 = 0; s0 < n; s0 += 64) M = fmaxf(M, s0 + lane < n ? ml_of(s0 + lane).x : none);
+  // eight planes' O at a time, the first of them on their way with the maxima
+  vecf v[8];
+  auto load = [&](int sp) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = o_of(sp + u < n ? sp + u : n - 1);
+  };
+  float2 p = lane < n ? ml_of(lane) : make_float2(none, 0.0f);
+  if (n > 0) load(0);
+  float M = p.x;
+  for (int s0 = 64; s0 < n; s0 += 64) M = fmaxf(M, s0 + lane < n ? ml_of(s0 + lane).x : none);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
   vecf o = {};
   float L = 0.0f;
   for (int s0 = 0; s0 < n; s0 += 64) {
-    const float2 p = s0 + lane < n ? ml_of(s0 + lane) : make_float2(none, 0.0f);
+    if (s0 > 0) p = s0 + lane < n ? ml_of(s0 + lane) : make_float2(none, 0.0f);
     const float w = p.y > 0.0f ? __builtin_amdgcn_exp2f((p.x - M) * mscale) : 0.0f;  // 0: no visible key in that part
     L += w * p.y;
     const int m = n - s0 < 64 ? n - s0 : 64;
     for (int u0 = 0; u0 < m; u0 += 8) {
-      vecf v[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = o_of(s0 + (u0 + u < m ? u0 + u : m - 1));
+      if (s0 + u0 > 0) load(s0 + u0);
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         // (a part without a visible key leaves its O row unwritten)
@@ -122,7 +130,7 @@ __global__ __launch_bounds__(256) void join_planes(const JoinArgs a) {
 #pragma unroll
   for (int s = 1; s < 64; s <<= 1) L += __shfl_xor(L, s);
   const float inv = L > 0.0f ? 1.0f / L : 0.0f;
-  T* orow = reinterpret_cast<T*>(a.out) + row * D + lane * PL;
+  T* orow = reinterpret_cast<T*>(a.out) + int64_t(row) * D + lane * PL;
 #pragma unroll
   for (int j = 0; j < PL; ++j) orow[j] = T(o[j] * inv);
   if (a.lse && lane == 0) a.lse[at.at2] = L > 0.0f ? M / sqrtf((float)D) + logf(L) : none;
@@ -132,7 +140,8 @@ constexpr int kWidePlanes = 4;
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void join_rows(const JoinArgs a) {
-  const int64_t row = int64_t(blockIdx.x) * 16 + threadIdx.x / 16, rows = int64_t(a.batch) * a.n_q * a.heads;
+  const int64_t rows = int64_t(a.batch) * a.n_q * a.heads;
+  const uint32_t row = blockIdx.x * 16 + threadIdx.x / 16;
   const int l16 = threadIdx.x % 16, n = a.n_prefix + a.n_own;
   if (row >= rows) return;
   const JoinRow at = join_row(a, row);
@@ -169,7 +178,7 @@ __global__ __launch_bounds__(256) void join_rows(const JoinArgs a) {
   vect r;
 #pragma unroll
   for (int j = 0; j < PL; ++j) r[j] = T(o[j] * inv);
-  *reinterpret_cast<vect*>(reinterpret_cast<T*>(a.out) + row * D + l16 * PL) = r;
+  *reinterpret_cast<vect*>(reinterpret_cast<T*>(a.out) + int64_t(row) * D + l16 * PL) = r;
   if (a.lse && l16 == 0) a.lse[at.at2] = L > 0.0f ? M / sqrtf((float)D) + logf(L) : -__builtin_inff();
 }
 
@@ -179,7 +188,7 @@ hipError_t launch_join_d(const JoinArgs& a, hipStream_t s) {
   // 16 lanes a row from four rows for every SIMD on
   const bool wide = a.n_prefix + a.n_own <= kWidePlanes && rows >= 4096;
   const int64_t wgs = (rows + (wide ? 15 : 3)) / (wide ? 16 : 4);
-  if (wgs > 0x7fffffff) return hipErrorInvalidValue;
+  if (rows > 0x7fffffff) return hipErrorInvalidValue;  // (their planes would be 500 GB)
   if (wide) hipLaunchKernelGGL((join_rows<T, D>), dim3((unsigned)wgs), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((join_planes<T, D>), dim3((unsigned)wgs), dim3(256), 0, s, a);
   return hipGetLastError();
