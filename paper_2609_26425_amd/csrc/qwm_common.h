@@ -173,6 +173,7 @@ struct RotaryArgs {
   void *q_out, *k_out;
   const int32_t* pos;  // [tokens][3], or NULL: token i of a batch entry is pos0 + i of the frame grid
   int64_t pos0, n, tokens, token_stride;
+  int block_tokens;        // tokens of a workgroup
   int heads, pairs;        // turned pairs of a head
   int end_t, end_h;        // pairs [0, end_t) turn by time, [end_t, end_h) by height, the rest by width
   int height, width;

@@ -7,15 +7,15 @@
 // more than fp32: turns = x f / 2 pi is formed and reduced to [-1/2, 1/2] in fp64,
 // and only the remainder goes to fp32 (2^-25 of a turn), so the cosines are right
 // to fp32 for any position. Memory bound: every value is read once and written
-// once. Queries and Keys of 4,680 tokens x 40 heads x 128: 192 MB in 41.5 us, 4.6 TB/s
-// (a copy of as many bytes: 5.2). Four tokens a workgroup are 1,170 workgroups there, and a
-// single token's launch is one: 6.4 us from call to end, 2.2 of them the kernel.
+// once. Queries and Keys of 4,680 tokens x 40 heads x 128: 192 MB in 38.9 us, 4.9 TB/s
+// (a copy of as many bytes: 5.2). A single token's launch is one workgroup: 6.2 us from
+// call to end, 2.2 of them the kernel.
 #include "qwm_common.h"
 
 namespace qwm {
 namespace {
 
-constexpr int kRotThreads = 256;
+constexpr int kRotThreads = 256, kRotTokens = 8;  // of a workgroup, at most
 
 template <typename T>
 struct Vec16 {  // 16 bytes of T as floats
@@ -57,17 +57,17 @@ __device__ inline uint4 pack(const Vec16<T>& v) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// TT tokens per workgroup. HALVES: pair p is channels (p, p + pairs), so a thread
+// a.block_tokens tokens per workgroup. HALVES: pair p is channels (p, p + pairs), so a thread
 // holds a vector of each half; otherwise it is channels (2 p, 2 p + 1) of one vector.
 // Channels past the turned pairs (p >= pairs) are copied (a product with cos 1 and sin 0
 // would lose the sign of a zero, and take a pair's second infinity into its first).
-template <typename T, int D, bool HALVES, int TT>
+template <typename T, int D, bool HALVES>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(const RotaryArgs a) {
   constexpr int P = D / 2, N = Vec16<T>::N, UNIT = HALVES ? 2 * N : N, UNITS = D / UNIT;
   constexpr int VN = HALVES ? 2 : 1;  // vectors of a unit
-  __shared__ __attribute__((aligned(16))) float2 cs[TT * P];
-  const int64_t tok0 = int64_t(blockIdx.x) * TT;
-  const int tokens = int(a.tokens - tok0 < TT ? a.tokens - tok0 : TT);
+  __shared__ __attribute__((aligned(16))) float2 cs[kRotTokens * P];
+  const int64_t tok0 = int64_t(blockIdx.x) * a.block_tokens;
+  const int tokens = int(a.tokens - tok0 < a.block_tokens ? a.tokens - tok0 : a.block_tokens);
   const int row = a.heads * UNITS, total = tokens * row;
   const int64_t out_stride = int64_t(a.heads) * D;
   struct Unit {
@@ -168,9 +168,16 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(const RotaryArgs a)
 
 template <typename T, int D, bool HALVES>
 hipError_t launch_t(const RotaryArgs& a, hipStream_t s) {
-  constexpr int TT = 4;
-  hipLaunchKernelGGL((rotary_kernel<T, D, HALVES, TT>), dim3((unsigned)((a.tokens + TT - 1) / TT)), dim3(kRotThreads), 0, s,
-                     a);
+  // A token a workgroup from half a unit a thread on: many small workgroups even out over
+  // the CUs (d = 128, BF16, us with 1 / 2 / 4 tokens: 4 x 3,120 tokens of 30 heads 70 / 77 / 85,
+  // 50,000 of 8 heads 70 / 73 / 77). Fewer heads take more, for their angles and their
+  // workgroup's start (100,000 of 4 heads 94 / 72 / 74; 200,000 of 2 heads at d = 64 with 1 / 4
+  // / 8 155 / 53 / 41).
+  RotaryArgs b = a;
+  const int units = a.heads * (D * int(sizeof(T)) / (HALVES ? 32 : 16)), fill = kRotThreads / 2 / units;
+  b.block_tokens = fill < 1 ? 1 : (fill < kRotTokens ? fill : kRotTokens);
+  hipLaunchKernelGGL((rotary_kernel<T, D, HALVES>), dim3((unsigned)((a.tokens + b.block_tokens - 1) / b.block_tokens)),
+                     dim3(kRotThreads), 0, s, b);
   return hipGetLastError();
 }
 
