@@ -754,32 +754,41 @@ quantwm_status quantwm_attend_shared(const quantwm_config* prefix_cfg, const voi
       return fail(QWM_ERR_INVALID_ARG, "workspace too small: %zu < %zu bytes", workspace_bytes, need);
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
-  hipError_t e;
-  // one pass: its partial planes at `at`
-  auto pass = [&](const quantwm_config* f, qwm::AttendArgs& a, bool few, int planes, int64_t n_keys, void* at) {
-    if (few && qwm::attend_few_plan(a, f->batch, device_cus(), qwm::elem_bytes(*f), planes)) {
-      set_planes(f, a, a.n_split, at);
-      return qwm::launch_attend_few(a, f->head_dim, qwm::elem_bytes(*f), f->batch, s);
-    }
-    set_planes(f, a, qwm::attend_splits(a.n_q, f->heads, f->batch, n_keys, device_cus(), qwm::elem_bytes(*f)), at);
-    return launch_attend(f, a, false, s);
+  // the parts of one pass and their planes at `at`; whether they are the few-row kernel's
+  auto plan = [&](const quantwm_config* f, qwm::AttendArgs& a, bool few, int planes, int64_t n_keys, void* at) {
+    few = few && qwm::attend_few_plan(a, f->batch, device_cus(), qwm::elem_bytes(*f), planes);
+    set_planes(f, a, few ? a.n_split : qwm::attend_splits(a.n_q, f->heads, f->batch, n_keys, device_cus(), qwm::elem_bytes(*f)), at);
+    return few;
+  };
+  auto launch = [&](const quantwm_config* f, const qwm::AttendArgs& a, bool few) {
+    return few ? qwm::launch_attend_few(a, f->head_dim, qwm::elem_bytes(*f), f->batch, s) : launch_attend(f, a, false, s);
   };
   qwm::JoinArgs c{};
   c.n_q = n_q; c.heads = cfg->heads; c.batch = cfg->batch; c.out = out; c.lse = lse_out;
+  qwm::AttendArgs pre, own;
+  bool few_pre = false, few_own = false;
   if (p.prefix > 0) {
-    qwm::AttendArgs a = attend_args(prefix_cfg, prefix_calibs, n_epochs, epoch_start, prefix_cache, n_prefix, nullptr,
-                                    nullptr, 0, q, n_q * cfg->batch, n_prefix, 1, nullptr, nullptr, nullptr);
-    if ((e = pass(prefix_cfg, a, p.few_prefix, p.prefix, n_prefix, workspace)) != hipSuccess)
-      return hip_fail(e, "attend launch (prefix)");
-    c.prefix_o = a.part_o; c.prefix_ml = a.part_ml; c.n_prefix = a.n_split;
+    pre = attend_args(prefix_cfg, prefix_calibs, n_epochs, epoch_start, prefix_cache, n_prefix, nullptr, nullptr, 0, q,
+                      n_q * cfg->batch, n_prefix, 1, nullptr, nullptr, nullptr);
+    few_pre = plan(prefix_cfg, pre, p.few_prefix, p.prefix, n_prefix, workspace);
+    c.prefix_o = pre.part_o; c.prefix_ml = pre.part_ml; c.n_prefix = pre.n_split;
   }
   if (p.own > 0) {
-    qwm::AttendArgs a = attend_args(cfg, calib, 1, nullptr, cache, n_cache, k_act, v_act, n_act, q, n_q,
-                                    q_start - n_prefix, frame_tokens, nullptr, nullptr, nullptr);
-    if ((e = pass(cfg, a, p.few_own, p.own, n_own, static_cast<uint8_t*>(workspace) + p.prefix_bytes)) != hipSuccess)
-      return hip_fail(e, "attend launch (own keys)");
-    c.own_o = a.part_o; c.own_ml = a.part_ml; c.n_own = a.n_split;
+    own = attend_args(cfg, calib, 1, nullptr, cache, n_cache, k_act, v_act, n_act, q, n_q, q_start - n_prefix,
+                      frame_tokens, nullptr, nullptr, nullptr);
+    few_own = plan(cfg, own, p.few_own, p.own, n_own, static_cast<uint8_t*>(workspace) + p.prefix_bytes);
+    c.own_o = own.part_o; c.own_ml = own.part_ml; c.n_own = own.n_split;
   }
+  hipError_t e = hipSuccess;
+  if (few_pre && few_own && qwm::attend_few_pairs(*prefix_cfg, *cfg)) {
+    // chains too short to fill the GPU, side by side (3 rollouts x 33 fp32 Queries over 777
+    // shared keys and 103 own ones: 23 us, one after the other 36)
+    e = qwm::launch_attend_few(pre, cfg->head_dim, qwm::elem_bytes(*cfg), 1, s, &own, cfg->batch);
+  } else {
+    if (p.prefix > 0) e = launch(prefix_cfg, pre, few_pre);
+    if (e == hipSuccess && p.own > 0) e = launch(cfg, own, few_own);
+  }
+  if (e != hipSuccess) return hip_fail(e, "attend launch");
   if ((e = qwm::launch_join(c, cfg->head_dim, cfg->dtype == QWM_BF16, s)) != hipSuccess)
     return hip_fail(e, "join launch");
   return ok();

@@ -37,14 +37,14 @@ struct F32Regs {
 };
 
 template <int D, int RP, bool SI8>
-__global__ __launch_bounds__(64 * kF32Waves) void attend_few_f32_kernel(const AttendArgs a) {
+__device__ __forceinline__ void few_f32(const AttendArgs& a, uint32_t place_l, uint32_t place_n) {
   typedef Mfma<float> MF;
   constexpr int NW = kF32Waves, CK = kFewChunk, HK = D / 2, W = D / 32;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
   const int Kc = a.n_centroids, r = a.rank, G = D / a.L.ng;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l32 = lane % 32,
             hf = lane / 32;
-  const FewPlace place = few_place(a, blockIdx.x, gridDim.x);
+  const FewPlace place = few_place(a, place_l, place_n);
   const int part = place.part, h = place.h, b = place.b;
   const int64_t bh = place.bh, n_bh = place.n_bh;
   const int qa = place.block * kFewQ, rows = min(kFewQ, int(a.n_q) - qa);
@@ -367,7 +367,20 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_few_f32_kernel(const At
 }
 
 template <int D, int RP, bool SI8>
-hipError_t launch_k(const AttendArgs& a, int batch, hipStream_t s) {
+__global__ __launch_bounds__(64 * kF32Waves) void attend_few_f32_kernel(const AttendArgs a) {
+  few_f32<D, RP, SI8>(a, blockIdx.x, gridDim.x);
+}
+
+// Both launches of a pair: a kernel of its own, since arguments at a computed address cost a
+// single launch 1.4 us.
+template <int D, int RP, bool SI8>
+__global__ __launch_bounds__(64 * kF32Waves) void attend_few_f32_pair(const FewPair two) {
+  const bool second = blockIdx.x >= two.n0;
+  few_f32<D, RP, SI8>(two.a[second ? 1 : 0], blockIdx.x - (second ? two.n0 : 0), second ? gridDim.x - two.n0 : two.n0);
+}
+
+template <int D, int RP, bool SI8>
+hipError_t launch_k(const AttendArgs& a, int batch, const AttendArgs* other, int other_batch, hipStream_t s) {
   // dynamic LDS: the tiles, and the merge in their place (32 rows of it are as large)
   constexpr size_t lds = size_t(kF32Waves) * (FewTile<D>::FLOATS + 2 * kFewQ) * 4;
   static_assert(lds <= kLdsLimit && FewTile<D>::FLOATS >= kFewQ * (D + 4), "the merge fits where the tiles were");
@@ -377,23 +390,29 @@ hipError_t launch_k(const AttendArgs& a, int batch, hipStream_t s) {
   if (e != hipSuccess) return e;
   const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
   if (!bit || !(raised.load(std::memory_order_acquire) & bit)) {
-    e = hipFuncSetAttribute((const void*)attend_few_f32_kernel<D, RP, SI8>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                            int(kLdsLimit));
-    if (e != hipSuccess) return e;
+    for (const void* f : {(const void*)attend_few_f32_kernel<D, RP, SI8>, (const void*)attend_few_f32_pair<D, RP, SI8>}) {
+      e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, int(kLdsLimit));
+      if (e != hipSuccess) return e;
+    }
     raised.fetch_or(bit, std::memory_order_release);
   }
-  const dim3 grid((unsigned)a.n_split * (unsigned)a.heads * (unsigned)(a.q_blocks * batch));
-  hipLaunchKernelGGL((attend_few_f32_kernel<D, RP, SI8>), grid, dim3(64 * kF32Waves), lds, s, a);
+  auto wgs = [](const AttendArgs& x, int n) { return uint32_t(x.n_split) * uint32_t(x.heads) * uint32_t(x.q_blocks * n); };
+  const uint32_t n0 = wgs(a, batch);
+  if (other)
+    hipLaunchKernelGGL((attend_few_f32_pair<D, RP, SI8>), dim3(n0 + wgs(*other, other_batch)), dim3(64 * kF32Waves), lds, s,
+                       FewPair{{a, *other}, n0});
+  else
+    hipLaunchKernelGGL((attend_few_f32_kernel<D, RP, SI8>), dim3(n0), dim3(64 * kF32Waves), lds, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 template <int D, int RP>
-hipError_t launch_attend_few_f32_rp(const AttendArgs& a, int batch, hipStream_t s) {
-  return a.L.i8 ? launch_k<D, RP, true>(a, batch, s) : launch_k<D, RP, false>(a, batch, s);
+hipError_t launch_attend_few_f32_rp(const AttendArgs& a, int batch, const AttendArgs* other, int other_batch, hipStream_t s) {
+  return a.L.i8 ? launch_k<D, RP, true>(a, batch, other, other_batch, s) : launch_k<D, RP, false>(a, batch, other, other_batch, s);
 }
 
-template hipError_t launch_attend_few_f32_rp<QWM_ATTEND_D, QWM_ATTEND_RP>(const AttendArgs&, int, hipStream_t);
+template hipError_t launch_attend_few_f32_rp<QWM_ATTEND_D, QWM_ATTEND_RP>(const AttendArgs&, int, const AttendArgs*, int, hipStream_t);
 
 }  // namespace qwm

@@ -218,11 +218,11 @@ hipError_t launch_d(const AttendArgs& a, int batch, bool logits, hipStream_t s) 
 }
 
 template <int D>
-hipError_t launch_few_f32_d(const AttendArgs& a, int batch, hipStream_t s) {
+hipError_t launch_few_f32_d(const AttendArgs& a, int batch, const AttendArgs* other, int other_batch, hipStream_t s) {
   hipError_t e;
-  if (a.rank == 0) e = launch_attend_few_f32_rp<D, 0>(a, batch, s);
-  else if (a.rank <= 16) e = launch_attend_few_f32_rp<D, 16>(a, batch, s);
-  else e = launch_attend_few_f32_rp<D, 32>(a, batch, s);
+  if (a.rank == 0) e = launch_attend_few_f32_rp<D, 0>(a, batch, other, other_batch, s);
+  else if (a.rank <= 16) e = launch_attend_few_f32_rp<D, 16>(a, batch, other, other_batch, s);
+  else e = launch_attend_few_f32_rp<D, 32>(a, batch, other, other_batch, s);
   if (e != hipSuccess || a.n_split == 1 || !a.out) return e;
   return launch_join_own<float, D>(a, batch, s);
 }
@@ -312,12 +312,20 @@ bool attend_few_plan(AttendArgs& a, int batch, int cus, int elem, int most) {
   return true;
 }
 
-hipError_t launch_attend_few(const AttendArgs& a, int d, int elem, int batch, hipStream_t s) {
+// (BF16 launches fill the GPU by themselves, and differ in their waves.)
+bool attend_few_pairs(const quantwm_config& a, const quantwm_config& b) {
+  auto pad = [](int r) { return (r + 15) / 16; };
+  return a.dtype == QWM_F32 && pad(a.rank) == pad(b.rank) && ((a.storage ^ b.storage) & QWM_STORE_SCALE_I8) == 0;
+}
+
+hipError_t launch_attend_few(const AttendArgs& a, int d, int elem, int batch, hipStream_t s, const AttendArgs* other,
+                             int other_batch) {
   if (elem == 4) {
-    if (d == 64) return launch_few_f32_d<64>(a, batch, s);
-    if (d == 128) return launch_few_f32_d<128>(a, batch, s);
+    if (d == 64) return launch_few_f32_d<64>(a, batch, other, other_batch, s);
+    if (d == 128) return launch_few_f32_d<128>(a, batch, other, other_batch, s);
     return hipErrorInvalidValue;
   }
+  if (other) return hipErrorInvalidValue;
   if (d == 64) return launch_few_d<64>(a, batch, s);
   if (d == 128) return launch_few_d<128>(a, batch, s);
   return hipErrorInvalidValue;

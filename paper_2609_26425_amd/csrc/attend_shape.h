@@ -50,6 +50,6 @@ hipError_t launch_attend_rp(const AttendArgs& a, int batch, bool logits, hipStre
 template <int D, int RP>
 hipError_t launch_attend_few_rp(const AttendArgs& a, int batch, hipStream_t s);
 template <int D, int RP>
-hipError_t launch_attend_few_f32_rp(const AttendArgs& a, int batch, hipStream_t s);
+hipError_t launch_attend_few_f32_rp(const AttendArgs& a, int batch, const AttendArgs* other, int other_batch, hipStream_t s);
 
 }  // namespace qwm

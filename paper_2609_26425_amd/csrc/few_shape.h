@@ -58,6 +58,12 @@ inline __host__ __device__ FewSegment few_segment_of(const AttendArgs& a, int i,
   return few_segment(lo, end, act, r);
 }
 
+// Two launches of one kernel instance as one: workgroups [0, n0) run the first.
+struct FewPair {
+  AttendArgs a[2];
+  uint32_t n0;
+};
+
 #ifdef __HIPCC__
 // What workgroup L of n runs, in a launch of n_split parts of every unit (a Query block of
 // a head). Two orders:

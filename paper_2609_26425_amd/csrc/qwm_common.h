@@ -206,7 +206,11 @@ hipError_t launch_attend_bf16(const AttendArgs& a, int d, int batch, bool logits
 bool attend_few_takes(const quantwm_config& c, int64_t n_q, int64_t n_keys);
 int attend_few_planes(int64_t n_q, int heads, int batch, int64_t n_keys, int cus, int elem);
 bool attend_few_plan(AttendArgs& a, int batch, int cus, int elem, int most);
-hipError_t launch_attend_few(const AttendArgs& a, int d, int elem, int batch, hipStream_t s);
+// other: a second launch, of planes too, that runs beside the first one in the same grid
+// (attend_few_pairs: their kernel instances agree).
+hipError_t launch_attend_few(const AttendArgs& a, int d, int elem, int batch, hipStream_t s, const AttendArgs* other = nullptr,
+                             int other_batch = 0);
+bool attend_few_pairs(const quantwm_config& a, const quantwm_config& b);
 hipError_t launch_join(const JoinArgs& a, int d, bool bf16_out, hipStream_t s);
 hipError_t launch_rotary(const RotaryArgs& a, int d, bool bf16_data, bool halves, hipStream_t s);
 size_t attend_lds_bytes(int d, int elem, int rank, int n_centroids, bool tables_in_lds);

@@ -30,6 +30,14 @@ CASES = {
     "few-own-wide": (2, 2, 128, "bf16", ([0], 500, 200, 32, 16, 0), (400, 1, 250, 32, 32, 1), 1, 300, 1),
     "f32": (3, 2, 64, "f32", ([0, 99], 700, 16, 32, 4, 0), (70, 33, 16, 32, 4, 0), 1, 70, 33),
     "f32-128": (2, 2, 128, "f32", ([0], 200, 16, 32, 32, 1), (65, 0, 16, 16, 8, 0), 20, 45, 40),
+    # more heads than CUs: parts in the order of their segments
+    "many-rollouts": (70, 4, 64, "bf16", ([0, 64], 150, 16, 32, 8, 0), (40, 3, 16, 32, 4, 0), 1, 41, 2),
+    "f32-many-rollouts": (40, 8, 64, "f32", ([0, 64], 150, 16, 32, 8, 0), (40, 3, 16, 32, 4, 0), 1, 41, 2),
+    # fp32 passes that share a grid, in two formats, and that do not (ranks, scales)
+    "f32-two-formats": (4, 3, 64, "f32", ([0, 64, 200], 333, 37, 16, 12, 0), (130, 5, 8, 64, 3, 0), 2, 100, 9),
+    "f32-i8": (2, 2, 128, "f32", ([0], 300, 64, 32, 8, 1), (90, 0, 16, 16, 16, 1), 1, 60, 40),
+    "f32-ranks-apart": (2, 2, 64, "f32", ([0], 300, 16, 32, 20, 0), (90, 7, 16, 16, 0, 0), 1, 60, 40),
+    "f32-scales-apart": (2, 2, 64, "f32", ([0], 300, 16, 32, 8, 0), (90, 7, 16, 16, 8, 1), 1, 60, 40),
 }
 
 
