@@ -11,7 +11,7 @@
 //
 // Bound by its chain of loads, centroid gathers and products: with a chunk or two a wave
 // there is nothing to hide them behind. 2 heads x 257 Queries with 305 to 361 keys in reach
-// (d = 64, rank 4): 18 us and 4 for the merge, against 29 with 256-row workgroups.
+// (d = 64, rank 4): 13 us and 4 for the merge, against 29 with 256-row workgroups.
 #include "attend_device.h"
 #include "attend_shape.h"
 #include "few_shape.h"
@@ -20,6 +20,8 @@
 
 namespace qwm {
 namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kF32Waves = 4;
 
@@ -148,6 +150,26 @@ __device__ __forceinline__ void few_f32(const AttendArgs& a, uint32_t place_l, u
     for (int st = 0; st < HK / 4; ++st) uv[st] = reinterpret_cast<const float4*>(urow)[st];
   }
   __builtin_amdgcn_sched_barrier(0);
+  // both centroid rows of a chunk's keys are gathered before either is used (d = 64; the
+  // registers of d = 128 hold one side at a time), the first ones while q U_r is made
+  constexpr bool BOTH = W == 2;
+  float muk[W][16], muv[W][16];
+  auto gather = [&](const float* row, float (&mu)[W][16]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < W; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 v = reinterpret_cast<const float4*>(row + 16 * u)[i];
+        mu[u][4 * i] = v.x; mu[u][4 * i + 1] = v.y; mu[u][4 * i + 2] = v.z; mu[u][4 * i + 3] = v.w;
+      }
+  };
+  auto gather_keys = [&]() __attribute__((always_inline)) { gather(gK + int64_t(int(P.k_id) < Kc ? int(P.k_id) : Kc - 1) * D, muk); };
+  auto gather_first = [&]() __attribute__((always_inline)) {
+    gather(gV + int64_t(int(P.v_id) < Kc ? int(P.v_id) : Kc - 1) * D, muv);
+    if constexpr (BOTH) gather_keys();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  if (!act && t0 < t1) gather_first();
 #pragma unroll
   for (int st = 0; st < HK / 4; ++st) {
     q[4 * st] = qvalid ? qv[st].x : 0.0f;
@@ -244,25 +266,8 @@ __device__ __forceinline__ void few_f32(const AttendArgs& a, uint32_t place_l, u
     };
     for (int t = t0 + wave; t < t1; t += NW) {
       const int k0 = key_of(t);
-      const float* mk = gK + int64_t(int(P.k_id) < Kc ? int(P.k_id) : Kc - 1) * D;
-      const float* mv = gV + int64_t(int(P.v_id) < Kc ? int(P.v_id) : Kc - 1) * D;
+      if (t > t0 + wave) gather_first();
       const bool in = k0 + l32 >= g.lo;  // not a key of the neighbouring epoch before the segment's first
-      // both centroid rows are gathered before either is used (d = 64; the registers of
-      // d = 128 hold one side at a time)
-      constexpr bool BOTH = W == 2;
-      float muk[W][16], muv[W][16];
-      auto gather = [&](const float* row, float (&mu)[W][16]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < W; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 v = reinterpret_cast<const float4*>(row + 16 * u)[i];
-            mu[u][4 * i] = v.x; mu[u][4 * i + 1] = v.y; mu[u][4 * i + 2] = v.z; mu[u][4 * i + 3] = v.w;
-          }
-      };
-      gather(mv, muv);
-      if constexpr (BOTH) gather(mk, muk);
-      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int u = 0; u < W; ++u) {
         float x[16];
@@ -271,7 +276,7 @@ __device__ __forceinline__ void few_f32(const AttendArgs& a, uint32_t place_l, u
 #pragma unroll
         for (int i = 0; i < 4; ++i) row[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
       }
-      if constexpr (!BOTH) gather(mk, muk);
+      if constexpr (!BOTH) gather_keys();
       f32x16 s;
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = 0.0f;
@@ -339,27 +344,33 @@ __device__ __forceinline__ void few_f32(const AttendArgs& a, uint32_t place_l, u
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < rows * D; i += 64 * NW) {
-    const int row = i / D, c = i % D;
+  for (int i = threadIdx.x; i < rows * (D / 4); i += 64 * NW) {
+    const int row = i / (D / 4), c = i % (D / 4) * 4;
     float M = -__builtin_inff();
 #pragma unroll
     for (int w = 0; w < NW; ++w) M = fmaxf(M, ml[2 * (w * rows + row)]);
-    float o = 0.0f, l = 0.0f;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    float l = 0.0f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       const float lw = ml[2 * (w * rows + row) + 1];
       const float e = lw > 0.0f ? __builtin_amdgcn_exp2f((ml[2 * (w * rows + row)] - M) * mscale) : 0.0f;
+      const f32x4 ow = *reinterpret_cast<const f32x4*>(mo + (w * rows + row) * OS + c);
       l += e * lw;
-      o += e * mo[(w * rows + row) * OS + c];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] += e * ow[j];
     }
     if (a.part_o) {
-      a.part_o[((int64_t(part) * n_bh + bh) * a.n_q + qa + row) * D + c] = o;
+      *reinterpret_cast<f32x4*>(a.part_o + ((int64_t(part) * n_bh + bh) * a.n_q + qa + row) * D + c) = o;
       if (c == 0) {
         plane_ml[2 * row] = M;
         plane_ml[2 * row + 1] = l;
       }
     } else {
-      reinterpret_cast<float*>(a.out)[((int64_t(b) * a.n_q + qa + row) * a.heads + h) * D + c] = l > 0.0f ? o / l : 0.0f;
+      f32x4 r;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r[j] = l > 0.0f ? o[j] / l : 0.0f;
+      *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + ((int64_t(b) * a.n_q + qa + row) * a.heads + h) * D + c) = r;
       if (a.lse && c == 0)
         a.lse[bh * a.n_q + qa + row] = l > 0.0f ? M / sqrtf((float)D) + logf(l) : -__builtin_inff();
     }

@@ -259,11 +259,12 @@ int few_parts(const AttendArgs& a, int64_t cpp, int64_t* chunks) {
   return int(most);
 }
 
-// Parts a launch asks for: one workgroup per CU (fp32: two, of four waves), and at least
-// a chunk for every wave. Launches of one chunk a wave stay one part.
+// Parts a launch asks for: one workgroup per CU, and at least a chunk for most waves
+// (launches of one chunk a wave stay one part); fp32: two workgroups, of four waves, per
+// CU, in which no wave has a chunk more than it must (attend_few_plan).
 int64_t few_want(int64_t n_q, int heads, int batch, int64_t chunks, int cus, int elem) {
   const int64_t wgs = (n_q + kFewQ - 1) / kFewQ * heads * batch, parts = (elem == 4 ? 2 * cus : cus) / wgs,
-                most = chunks <= (elem == 4 ? 4 : 12) ? 1 : chunks / (elem == 4 ? 4 : 8);
+                most = elem == 4 ? (chunks + 3) / 4 : (chunks <= 12 ? 1 : chunks / 8);
   const int64_t w = parts < most ? parts : most;
   return w > 1 ? w : 1;
 }
@@ -279,13 +280,13 @@ bool attend_few_takes(const quantwm_config& c, int64_t n_q, int64_t n_keys) {
   // tiled: 1 Query x 300 keys 13 / 15, x 30,000 33 / 55; 16 x 1,000 20 / 18, x 8,000 27 / 28, x
   // 30,000 37 / 56; 32 x 4,000 28 / 24, x 30,000 44 / 56; two blocks are never faster).
   if (c.dtype == QWM_BF16) return c.rank % 4 == 0 && n_q <= kFewQ && n_keys >= 384 * (n_q - 1);
-  // fp32: up to about 16 (d = 128: 6) products of 32 Queries x 32 keys a SIMD; beyond, blocks of
-  // 256 rows decode less (d = 64, us here / tiled: 2 heads x 257 Queries x 362 keys 18 / 29; 8 x
-  // 512 x 3,000 59 / 61; 8 x 1,024 x 3,000 95 / 89. d = 128: 2 x 257 x 362 27 / 48, 2 x 1,024 x
-  // 3,000 82 / 92, 8 x 1,024 x 1,024 94 / 78).
+  // fp32: up to nine products of 32 Queries x 32 keys a SIMD; beyond, blocks of 256 rows
+  // decode less (us here / tiled, d = 64: 2 heads x 257 Queries x 362 keys 16 / 29; 8 x 257 x
+  // 4,000 61 / 66; 8 x 512 x 4,000 83 / 70; d = 128: 23 / 48; 105 / 110; 150 / 114. The worst
+  // below the limit, 30 x 128 x 1,500, 48 / 39 and 79 / 63).
   // (a launch without keys still has its blocks, a grid dimension)
   const double units = double((n_q + kFewQ - 1) / kFewQ) * c.heads * c.batch * double(n_keys / kFewChunk + 1);
-  return n_q <= 4096 && units <= (c.head_dim == 64 ? 16384 : 6144);
+  return n_q <= 4096 && units <= 9216;
 }
 
 int attend_few_planes(int64_t n_q, int heads, int batch, int64_t n_keys, int cus, int elem) {
@@ -301,6 +302,9 @@ bool attend_few_plan(AttendArgs& a, int batch, int cus, int elem, int most) {
   const int64_t want = few_want(a.n_q, a.heads, batch, chunks, cus, elem);
   int64_t cpp = (chunks + want - 1) / want;
   if (cpp < 1) cpp = 1;
+  // fp32: whole rounds of the four waves, since a part takes as long as its first wave (14
+  // chunks in parts of 4 instead of 5, whose first wave has a second one to do: 5 us less)
+  if (elem == 4) cpp = (cpp + 3) / 4 * 4;
   int parts = few_parts(a, cpp, nullptr);
   while (parts > most && cpp < chunks) {
     cpp *= 2;
