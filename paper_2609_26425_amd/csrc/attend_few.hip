@@ -21,9 +21,9 @@
 //
 // Bound by vector issue and by latency at three waves a SIMD: some 520 vector instructions
 // for 32 keys (d = 128, rank 16), against 18 matrix products. One Query of 40 heads over
-// 15,600 keys of a cache of 32,760 (128 centroids): 34.3 us. 1,024 keys take 16 of that
+// 15,600 keys of a cache of 32,760 (128 centroids): 33.9 us. 1,024 keys take 16 of that
 // (the call, the staging of the tables, the merges), the rest is 1.3 ns a key of all
-// heads, 3.2 TB/s of packed fields. 256-row workgroups of attend.hip: 84 us.
+// heads, 3.2 TB/s of packed fields. 256-row workgroups of attend.hip: 75 us.
 #include "attend_device.h"
 #include "attend_shape.h"
 #include "few_shape.h"

@@ -73,7 +73,7 @@ struct FewPair {
 //   - units enough for every CU, so that a part is a whole segment: part by part, the
 //     first segments of all units before the second. The exact chunk's parts, often a few
 //     keys, then fill in behind the packed ones instead of standing between them (16
-//     rollouts x 30 heads, 130 packed keys and one exact: 30 -> 21 us).
+//     rollouts x 30 heads, 130 packed keys and one exact: 30 -> 22 us).
 struct FewPlace {
   int part, h, b, block;
   int64_t bh, n_bh;
