@@ -845,6 +845,7 @@ quantwm_status quantwm_rotary(const quantwm_config* cfg, const quantwm_rotary_ax
   QWM_TRY(check_dev(k, "k", false));
   QWM_TRY(check_dev(k_out, "k_out", false));
   const int elem = qwm::elem_bytes(*cfg);
+  if (row > (int64_t(1) << 30)) return fail(QWM_ERR_UNSUPPORTED, "heads * head_dim above 2^30");
   if (token_stride < row || token_stride * elem % 16 || token_stride > (int64_t(1) << 40))
     return fail(QWM_ERR_INVALID_ARG, "token_stride must be at least heads * head_dim and a multiple of 16 bytes");
   if (n > kMaxPositions / cfg->batch) return fail(QWM_ERR_UNSUPPORTED, "more than %lld tokens", (long long)kMaxPositions);

@@ -76,7 +76,8 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(const RotaryArgs a)
   constexpr int P = D / 2, N = Vec16<T>::N, UNIT = HALVES ? 2 * N : N, UNITS = D / UNIT;
   constexpr int VN = HALVES ? 2 : 1;  // vectors of a unit
   __shared__ __attribute__((aligned(16))) float2 cs[kRotTokens * P];
-  const int64_t tok0 = int64_t(blockIdx.x) * a.block_tokens;
+  const int64_t tok0 = (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * a.block_tokens;
+  if (tok0 >= a.tokens) return;
   const int tokens = int(a.tokens - tok0 < a.block_tokens ? a.tokens - tok0 : a.block_tokens);
   const int row = a.heads * UNITS, total = tokens * row;
   const int64_t out_stride = int64_t(a.heads) * D;
@@ -186,8 +187,10 @@ hipError_t launch_t(const RotaryArgs& a, hipStream_t s) {
   RotaryArgs b = a;
   const int units = a.heads * (D * int(sizeof(T)) / (HALVES ? 32 : 16)), fill = kRotThreads / 2 / units;
   b.block_tokens = fill < 1 ? 1 : (fill < kRotTokens ? fill : kRotTokens);
-  hipLaunchKernelGGL((rotary_kernel<T, D, HALVES>), dim3((unsigned)((a.tokens + b.block_tokens - 1) / b.block_tokens)),
-                     dim3(kRotThreads), 0, s, b);
+  // rows of 2^16 workgroups: a grid dimension holds fewer than 2^32 threads
+  const int64_t wgs = (a.tokens + b.block_tokens - 1) / b.block_tokens, x = wgs < 65536 ? wgs : 65536;
+  hipLaunchKernelGGL((rotary_kernel<T, D, HALVES>), dim3((unsigned)x, (unsigned)((wgs + x - 1) / x)), dim3(kRotThreads), 0, s,
+                     b);
   return hipGetLastError();
 }
 

@@ -155,3 +155,24 @@ def test_channels_past_the_axes_are_copied(halves, dims, dtype):
     bits = torch.int16 if dtype == "bf16" else torch.int32
     assert torch.equal(out[..., sum(dims):].view(bits), x[..., sum(dims):].view(bits))
     assert out[..., : sum(dims)].isfinite().all()
+
+
+def test_more_tokens_than_a_grid_dimension():
+    """A workgroup a token, past 2^24 of them (34 GB, in place): the first and last tokens
+    equal those of short calls."""
+    cfg = qw.make_config(1, 16, 64, 16, 16, 0, 1, 1, "bf16")
+    axes = qw.rotary_axes(cfg, (24, 20, 20), *GRID)
+    n = (1 << 24) + 70_003
+    if torch.cuda.mem_get_info()[0] < 3 * n * 16 * 64:
+        pytest.skip("needs 50 GB of device memory")
+    x = torch.empty(1, n, 16, 64, dtype=torch.bfloat16, device=DEV)
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    few = torch.randn(1, 9, 16, 64, generator=gen, device=DEV).bfloat16()
+    at = [0, 65_530, (1 << 24) - 4, (1 << 24) + 65_531, n - 9]
+    for i in at:
+        x[:, i:i + 9] = few
+    qw.quantwm_rotary(cfg, axes, x, None, n, x, pos0=11)
+    for i in at:
+        want = torch.empty_like(few)
+        qw.quantwm_rotary(cfg, axes, few, None, 9, want, pos0=11 + i)
+        assert torch.equal(x[:, i:i + 9], want)

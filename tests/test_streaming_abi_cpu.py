@@ -219,3 +219,8 @@ def test_window_without_keys_over_many_blocks():
 def test_rotary_refuses_what_overflows(kw, word):
     assert _rotary(**kw) == qw.ERR_INVALID_ARG
     assert word in qw.quantwm_last_error()
+
+
+def test_rotary_refuses_rows_past_its_counters():
+    assert _rotary(cfg=_cfg(heads=1 << 24), n=1, stride=1 << 31) == qw.ERR_UNSUPPORTED
+    assert "2^30" in qw.quantwm_last_error()
