@@ -386,7 +386,7 @@ typedef struct {
   int32_t dims[3];       /* channels of the time, height and width axes: even, summing to at most
                             head_dim (QWM_ROTARY_HALVES: to a multiple of 16) */
   int32_t height, width; /* rows and columns of a frame's tokens, for positions from the frame grid */
-  double freq[64];       /* radians per unit of position of every pair */
+  double freq[64];       /* radians per unit of position of every pair (finite also times 2^31) */
 } quantwm_rotary_axes;
 
 /* Fills *out with freq = base^(-2 i / D) for pair i of an axis with D channels. */
@@ -403,7 +403,8 @@ quantwm_status quantwm_rotary_init(const quantwm_config* cfg, const int32_t* dim
  * (pos0 + i) / (height width), then row and column inside the frame (each below
  * 2^31). inverse != 0 turns back by the same angles: the transpose of the turn, so
  * the gradient with respect to its input. Angles are formed in fp64 and the
- * products in fp32, with one rounding to the element type. n == 0 is a no-op. */
+ * products in fp32, with one rounding to the element type. n == 0 is a no-op.
+ * QWM_ERR_UNSUPPORTED when B n exceeds 0x7fff0000 or H * d 2^30. */
 quantwm_status quantwm_rotary(const quantwm_config* cfg, const quantwm_rotary_axes* axes, int64_t pos0,
                               const int32_t* pos, const void* q, const void* k, int64_t n, int64_t token_stride,
                               void* q_out, void* k_out, int32_t inverse, void* stream);
