@@ -229,9 +229,7 @@ __global__ __launch_bounds__(64 * few_waves(NQ, TAB)) void attend_few_kernel(con
     __builtin_amdgcn_sched_barrier(0);
   }
 
-  // ---- logits are in units of 2^qe of their Query: its binary16 copy holds q 2^(2 - qe),
-  // against Key residuals times 2^-2 (a step is a binary16 value, and three of them stay
-  // in its range)
+  // ---- logits are in units of 2^qe of their Query: its binary16 copy holds q 2^-qe
   float lscale[NQ], tau[NQ], unit[NQ];
   int qe[NQ], lim[NQ], wfrom[NQ];
   V qreg[NQ][ST], ureg[NQ];
@@ -244,7 +242,7 @@ __global__ __launch_bounds__(64 * few_waves(NQ, TAB)) void attend_few_kernel(con
 #pragma unroll
       for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(float(qf[n][st][j])));
     top = max_quarters(top);
-    qe[n] = int((__float_as_uint(top) >> 23) & 255) - 127 - 12;  // a zero Query: any unit
+    qe[n] = int((__float_as_uint(top) >> 23) & 255) - 127 - 14;  // a zero Query: any unit
     if (qe[n] < -100) qe[n] = -100;
     unit[n] = __uint_as_float(uint32_t(127 - qe[n]) << 23);      // 2^-qe
     lscale[n] = ldexpf(mscale, qe[n]);
@@ -257,8 +255,8 @@ __global__ __launch_bounds__(64 * few_waves(NQ, TAB)) void attend_few_kernel(con
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int c = st % 2 * 4 + j;
-        w[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(4.0f * unit[n] * float(qf[n][st & ~1][c]),
-                                                                       4.0f * unit[n] * float(qf[n][st | 1][c])));
+        w[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(unit[n] * float(qf[n][st & ~1][c]),
+                                                                       unit[n] * float(qf[n][st | 1][c])));
       }
       qreg[n][st] = act ? qf[n][st] : __builtin_bit_cast(V, make_uint4(w[0], w[1], w[2], w[3]));
     }
@@ -405,16 +403,12 @@ __global__ __launch_bounds__(64 * few_waves(NQ, TAB)) void attend_few_kernel(con
 #pragma unroll
         for (int n = 0; n < NQ; ++n) mu[e][n][i] = row[16 * n];
       }
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) s[e][n] = SI8 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : mu[e][n];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
+    // the residuals' products of one key, onto s; of its steps c, those that `pick` leaves
+    auto residual = [&](int e, auto pick) __attribute__((always_inline)) {
 #pragma unroll
       for (int u = 0; u < W; ++u) {
-        // SI8: the integers c (code - z), exact; else s 2^-2 (code - z)
-        const _Float16 c = SI8 ? scale_of(p.k_s[e], u) : scale_of(p.k_s[e], u) * (_Float16)0.25f;
+        // s (code - z), or the integers c (code - z) (SI8), exact
+        const _Float16 c = pick(scale_of(p.k_s[e], u));
         const f16x2 cc = {c, c}, zh = __builtin_bit_cast(f16x2, zero_of(p.k_z[e], kg0, u));
         uint32_t w[8];
 #pragma unroll
@@ -428,12 +422,14 @@ __global__ __launch_bounds__(64 * few_waves(NQ, TAB)) void attend_few_kernel(con
                 __builtin_bit_cast(f16x8, make_uint4(w[4 * x], w[4 * x + 1], w[4 * x + 2], w[4 * x + 3])),
                 __builtin_bit_cast(f16x8, qreg[n][2 * u + x]), s[e][n], 0, 0, 0);
       }
+    };
+    auto coefficients = [&](int e) __attribute__((always_inline)) {
       if constexpr (SI8) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const _Float16 sg = __builtin_bit_cast(_Float16, uint16_t(p.k_sg[2 * e + i / 2] >> (16 * (i % 2))));
 #pragma unroll
-          for (int n = 0; n < NQ; ++n) s[e][n][i] = __builtin_fmaf(s[e][n][i], 0.25f * (float)sg, mu[e][n][i]);
+          for (int n = 0; n < NQ; ++n) s[e][n][i] = __builtin_fmaf(s[e][n][i], (float)sg, mu[e][n][i]);
         }
       }
       if constexpr (RP > 0) {
@@ -451,6 +447,34 @@ __global__ __launch_bounds__(64 * few_waves(NQ, TAB)) void attend_few_kernel(con
         for (int n = 0; n < NQ; ++n)
           s[e][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V, make_uint4(w[0], w[1], w[2], w[3])), ureg[n],
                                                             s[e][n], 0, 0, 0);
+      }
+    };
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) s[e][n] = SI8 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : mu[e][n];
+      residual(e, [](_Float16 c) { return c; });
+      coefficients(e);
+    }
+    if constexpr (!SI8) {
+      // Steps of which three leave binary16's range (bits from 0x7555 on: the sum reaches a
+      // half's top bit), in no Keys of usual size: the chunk again, with these steps a
+      // quarter as large in products of their own. All the others stay as they are stored,
+      // since a smaller one's lowest bits have no room below binary16's normal range.
+      if (__any(((p.k_s[0] + 0x0aab0aabu) | (p.k_s[1] + 0x0aab0aabu)) & 0x80008000u)) {
+        auto large = [](_Float16 c) { return __builtin_bit_cast(uint16_t, c) >= 0x7555; };
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) s[e][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+          residual(e, [&](_Float16 c) { return large(c) ? c * (_Float16)0.25f : (_Float16)0; });
+#pragma unroll
+          for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[e][n][i] = __builtin_fmaf(s[e][n][i], 4.0f, mu[e][n][i]);
+          residual(e, [&](_Float16 c) { return large(c) ? (_Float16)0 : c; });
+          coefficients(e);
+        }
       }
     }
     load_key(p, next);

@@ -1,0 +1,150 @@
+"""The few-row attention kernels at the ends of their operands' ranges, and which of the
+two kernels a launch takes: against a plain 64-bit softmax over the Keys in one form only
+(as they decode for the few-row kernel, rounded to BF16 for the tiles), not in either."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import stream64 as s64
+from paper_2609_26425_amd import quantwm as qw
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def stream(rng, n, keys, mu, starts=(0,), batch=1, heads=2, d=128, kc=16, g=32, r=8, st=0, values=None, mu_v=None):
+    """n packed BF16 tokens: keys(rng, tables' mu_k, tokens) of tables mu(rng), Values likewise
+    (standard normal without `values`)."""
+    p = s64.Packed(rng, batch, heads, d, kc, g, r, "bf16", st, [0], 0, capacity=n)
+    p.n, p.starts, p.tables = n, list(starts), []
+    normal = lambda *s: rng.standard_normal(s)  # noqa: E731
+    for lo, hi in zip(p.starts, p.starts[1:] + [n]):
+        mk = s64.rounded(mu(rng, (batch, heads, kc, d)), "bf16")
+        mv = s64.rounded((mu_v or (lambda rng, s: normal(*s)))(rng, (batch, heads, kc, d)), "bf16")
+        u = np.stack([np.linalg.qr(normal(d, d))[0][:r] for _ in range(batch * heads)]).reshape(batch, heads, r, d)
+        t = (mk, mv, np.ones((batch, heads, d), np.float32), s64.rounded(u, "bf16"), np.ones((batch, heads, r), np.float32))
+        k = s64.rounded(keys(rng, mk, (batch, hi - lo, heads, d)), "bf16")
+        v = s64.rounded(normal(batch, hi - lo, heads, d) if values is None else values(rng, mv, (batch, hi - lo, heads, d)), "bf16")
+        oracle.append(p.ocfg, t, p.cache, lo, k, v)
+        p.tables.append(t)
+    return p
+
+
+def normal(size):
+    """Keys and tables of that size."""
+    return dict(keys=lambda rng, mk, s: size * rng.standard_normal(s), mu=lambda rng, s: size * rng.standard_normal(s))
+
+
+def members(rng, mu, s):
+    """Tokens that are centroids themselves: no residual."""
+    batch, n, heads, d = s
+    z = rng.integers(0, mu.shape[2], (batch, n, heads))
+    return mu[np.arange(batch)[:, None, None], np.arange(heads), z]
+
+
+def seen(n, n_q):
+    return np.arange(n) <= (n - n_q + np.arange(n_q))[:, None]
+
+
+def window(p, q, few, ka=None, va=None, workspace=True):
+    """quantwm_attend_window over everything, the Queries last: against the given form of
+    the Keys. Returns the results, and whether the other form fits too."""
+    B, n_q = q.shape[:2]
+    n_act = 0 if ka is None else ka.shape[1]
+    n = p.n + n_act
+    k, v = p.keys_values()
+    if n_act:
+        k, v = (np.concatenate([x, y.transpose(0, 2, 1, 3)], 2) for x, y in ((k, ka), (v, va)))
+    visible = seen(n, n_q)
+    refs = {}
+    for form in (False, True):
+        lg = p.logits(q, form)
+        if n_act:
+            lg = np.concatenate([lg, s64.exact_logits(q, ka)], 3)
+        refs[form] = (*s64.softmax(lg, visible, v), s64.tolerances(q, k, n, p.r, "bf16", p.residuals() if form else None))
+    nb = qw.quantwm_attend_window_workspace_bytes(p.cfg, p.n, n_act, n_q, 1, 0, n) if workspace else 0
+    ws = torch.empty(nb, dtype=torch.uint8, device=DEV) if nb else None
+    qd = s64.dev(q, torch.bfloat16)
+    kd, vd = (s64.dev(x, torch.bfloat16) if n_act else None for x in (ka, va))
+    out, lse = torch.full_like(qd, 7.0), torch.full((B, p.heads, n_q), 7.0, device=DEV)
+    qw.quantwm_attend_window(p.cfg, p.blocks(), p.starts, p.on_device(), p.n, kd, vd, n_act, qd, n_q, n - n_q, 1, 0, n,
+                             out, lse, ws)
+    torch.cuda.synchronize()
+    s64.check(out, lse, *refs[few])
+    try:
+        s64.check(out, lse, *refs[not few])
+    except AssertionError:
+        return out, lse, False
+    return out, lse, True
+
+
+def queries(rng, p, size, n_q, peaks=2.0):
+    """Queries of which three in four have most of their weight on one key."""
+    q = 0.5 / size * rng.standard_normal((p.batch, n_q, p.heads, p.d))
+    k = p.keys_values()[0]
+    for i in range(n_q):
+        if i % 4 != 3:
+            q[:, i] += peaks / size ** 2 * k[:, :, (37 * i + 5) % p.n]
+    return s64.rounded(q, "bf16")
+
+
+# Keys' size: steps from a few units of the last place of binary16's smallest values to such
+# that three of them pass its largest
+SIZES = [2.0 ** -23, 2.0 ** -20, 2.0 ** -18, 2.0 ** -16, 2.0 ** -14, 2.0 ** -12, 6000.0, 20000.0]
+SHAPES = {  # packed, exact keys, Queries, head_dim, group, rank, storage
+    "one": (1500, 0, 1, 128, 32, 8, 0), "one-act": (700, 9, 1, 64, 16, 4, 0), "some": (6500, 0, 16, 128, 16, 16, 0),
+    "wide": (7400, 3, 20, 64, 64, 0, 0), "wide-128": (7400, 0, 20, 128, 32, 32, 0), "some-i8": (1500, 0, 4, 128, 32, 8, 1),
+}
+
+
+@pytest.mark.parametrize("size", SIZES)
+@pytest.mark.parametrize("shape", list(SHAPES))
+def test_key_steps_of_any_size(shape, size):
+    n, n_act, n_q, d, g, r, st = SHAPES[shape]
+    rng = np.random.default_rng(n + int(np.log2(size)) % 64)
+    p = stream(rng, n, **normal(size), d=d, g=g, r=r, st=st)
+    res = np.abs(p.residuals())
+    assert res.max() > 65504.0 if size > 1e4 else size > 1 or st or 0 < res.max() < 8 * size  # at most three steps
+    q = queries(rng, p, size, n_q)
+    ka, va = (s64.rounded(x * rng.standard_normal((1, n_act, 2, d)), "bf16") if n_act else None for x in (size, 1.0))
+    window(p, q, True, ka, va)
+
+
+def test_key_steps_of_two_sizes_in_one_chunk():
+    """Every other token's steps times 3 pass binary16's range in the first channels; the
+    others are of size 1."""
+    rng, n, d = np.random.default_rng(1), 1500, 128
+    big = np.where(np.arange(d) < 64, 20000.0, 1.0)
+
+    def keys(rng, mk, s):
+        return rng.standard_normal(s) * np.where((np.arange(s[1]) % 2 == 0)[None, :, None, None], big, np.where(big > 1, 0, 1.0))
+
+    def mu(rng, s):
+        return rng.standard_normal(s) * np.where((np.arange(s[2]) % 2 == 0)[:, None], big, np.where(big > 1, 0, 1.0))
+    for n_q in (1, 3):
+        p = stream(rng, n, keys, mu)
+        q = s64.rounded(0.5 / np.where(big > 1, big, 1.0) * rng.standard_normal((1, n_q, 2, d)), "bf16")
+        window(p, q, True)
+
+
+@pytest.mark.parametrize("size", [2.0 ** -20, 2.0 ** -16, 20000.0])
+def test_shared_key_steps_of_any_size(size):
+    B, H, d, n_pre, n_own, n_q = 3, 2, 128, 1500, 700, 1
+    rng = np.random.default_rng(int(np.log2(size)) % 64)
+    pre, own = stream(rng, n_pre, **normal(size)), stream(rng, n_own, **normal(size), batch=B, g=16, r=4)
+    q = queries(rng, own, size, n_q)
+    q[1] = queries(rng, pre, size, n_q)[0]
+    (pk, pv), (k, v), flat = pre.keys_values(), own.keys_values(), q.reshape(1, B * n_q, H, d)
+    k, v = (np.concatenate([np.repeat(x, B, 0), y], 2) for x, y in ((pk, k), (pv, v)))
+    n = n_pre + n_own
+    lg = np.concatenate([pre.logits(flat, True).reshape(H, B, n_q, n_pre).transpose(1, 0, 2, 3), own.logits(q, True)], 3)
+    res = np.concatenate([np.repeat(pre.residuals(), B, 0), own.residuals()], 2)
+    ref = (*s64.softmax(lg, np.ones((n_q, n), bool), v), s64.tolerances(q, k, 2 * n + 64, 8, "bf16", res))
+    ws = torch.empty(qw.quantwm_attend_shared_workspace_bytes(pre.cfg, n_pre, own.cfg, n_own, 0, n_q), dtype=torch.uint8, device=DEV)
+    qd = s64.dev(q, torch.bfloat16)
+    out, lse = torch.full_like(qd, 7.0), torch.empty(B, H, n_q, device=DEV)
+    qw.quantwm_attend_shared(pre.cfg, pre.blocks(), [0], pre.on_device(), n_pre, own.cfg, own.blocks(), own.on_device(), n_own,
+                             None, None, 0, qd, n_q, n - 1, 1, out, lse, ws)
+    torch.cuda.synchronize()
+    s64.check(out, lse, *ref)
