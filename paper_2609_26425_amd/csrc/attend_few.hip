@@ -205,8 +205,9 @@ __global__ __launch_bounds__(64 * few_waves(NQ, TAB)) void attend_few_kernel(con
     load_row(reinterpret_cast<const bf16*>(a.q) +
                  ((int64_t(b) * a.n_q + qa + min(16 * n + l16, rows - 1)) * a.heads + h) * D + kq * HV, qf[n]);
   Regs P;
-  int ev = 0;  // Values are decoded times 2^-e_v, the exponent of their binary16 table
+  int ek = 0, ev = 0;  // Values are decoded times 2^-e_v, the exponent of their binary16 table
   if (!act) {
+    ek = reinterpret_cast<const int32_t*>(slab + a.o_e16)[0];
     ev = reinterpret_cast<const int32_t*>(slab + a.o_e16)[1];
     centroids(wave * 16);
     if constexpr (RP > 0) {
@@ -229,7 +230,10 @@ __global__ __launch_bounds__(64 * few_waves(NQ, TAB)) void attend_few_kernel(con
     __builtin_amdgcn_sched_barrier(0);
   }
 
-  // ---- logits are in units of 2^qe of their Query: its binary16 copy holds q 2^-qe
+  // ---- logits are in units of 2^qe of their Query: its binary16 copy holds q 2^-qe, with
+  // its largest magnitude in [2^14, 2^15) unless the Key table's, below 2^(15 + e_k), is past
+  // 2^104: q . mu, below 2^(23 + e_k) times the Query's, then stays below 2^126 in these units
+  // (the residuals, at most 3 x 65,504 a channel, are lost in such a sum)
   float lscale[NQ], tau[NQ], unit[NQ];
   int qe[NQ], lim[NQ], wfrom[NQ];
   V qreg[NQ][ST], ureg[NQ];
@@ -242,8 +246,8 @@ __global__ __launch_bounds__(64 * few_waves(NQ, TAB)) void attend_few_kernel(con
 #pragma unroll
       for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(float(qf[n][st][j])));
     top = max_quarters(top);
-    qe[n] = int((__float_as_uint(top) >> 23) & 255) - 127 - 14;  // a zero Query: any unit
-    if (qe[n] < -100) qe[n] = -100;
+    qe[n] = int((__float_as_uint(top) >> 23) & 255) - 127 + max(ek - 103, -14);
+    qe[n] = min(max(qe[n], -100), 120);  // a zero Query: any unit
     unit[n] = __uint_as_float(uint32_t(127 - qe[n]) << 23);      // 2^-qe
     lscale[n] = ldexpf(mscale, qe[n]);
     tau[n] = 8.0f / lscale[n];

@@ -148,3 +148,28 @@ def test_shared_key_steps_of_any_size(size):
                              None, None, 0, qd, n_q, n - 1, 1, out, lse, ws)
     torch.cuda.synchronize()
     s64.check(out, lse, *ref)
+
+
+@pytest.mark.parametrize("power,small", [(60, -60), (118, -118), (114, -86), (118, -90), (125, -97)])
+@pytest.mark.parametrize("n_q,few", [(1, True), (3, True), (20, True), (40, False)])
+def test_large_key_tables(power, small, n_q, few):
+    """Key centroids far out, and Queries as small or logits as large: all finite."""
+    rng = np.random.default_rng(power + n_q)
+    p = stream(rng, 7400 if n_q == 20 else 900, members, lambda rng, s: rng.uniform(-1.5, 1.5, s), r=4)
+    assert not p.residuals().any()  # so the packed tokens are those of the scaled tables too
+    p.tables = [(np.ldexp(t[0], power), *t[1:]) for t in p.tables]
+    q = s64.rounded(np.ldexp(0.5 * rng.standard_normal((1, n_q, 2, 128)), small), "bf16")
+    visible = seen(p.n, n_q)
+    lg = np.where(visible, p.logits(q, few), -np.inf)
+    top = lg.max(-1, keepdims=True)
+    first = lg > top - 2.0 ** -30 * np.abs(top)  # the best centroid's tokens
+    out, lse, _ = window(p, q, few)
+    assert out.isfinite().all() and lse.isfinite().all()
+    if power + small > 0:  # the mean Value of those tokens, where they lead by more than the logits err
+        qk = np.matmul(np.abs(q).transpose(0, 2, 1, 3), np.abs(p.keys_values()[0]).transpose(0, 1, 3, 2)).max() / 128 ** 0.5
+        led = top[..., 0] - np.where(first, -np.inf, lg).max(-1) > 4 * 140 * 2.0 ** -24 * qk + 100
+        assert led.mean() > 0.9
+        ref, _, mag = s64.softmax(np.where(first, 0.0, -np.inf), visible, p.keys_values()[1])
+        # their weights are equal: half a step of the result, and the sum's order
+        err = np.abs(out.double().cpu().numpy() - ref) - 2.0 ** -8 * np.abs(ref) - p.n * 2.0 ** -23 * mag
+        assert (err[led.transpose(0, 2, 1)] <= 0).all()
