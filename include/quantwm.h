@@ -148,9 +148,10 @@ size_t quantwm_calib_bytes(const quantwm_config* cfg);
  *   m           [d][d]  f32     Mn, only with QWM_METRIC_FULL (no bytes otherwise)
  *   mu_k16, mu_v16 [Kc][d] binary16  BF16 configs only (no bytes otherwise): the
  *                               centroids times 2^-e_k (2^-e_v), e the exponent that puts
- *                               the table's largest magnitude in [2^14, 2^15) (0 for an
- *                               all-zero table), rounded to binary16: exact for every
- *                               component of at least 2^-31 times that largest one
+ *                               the table's largest magnitude in [2^14, 2^15), at least
+ *                               -109 (0 for an all-zero table), rounded to binary16: exact
+ *                               for every component of at least 2^-31 times that largest
+ *                               one, and for all of a table that takes -109
  *   e16         [2]     int32   e_k, e_v (BF16 configs only)
  *   a_k3        [3][Kc][d] BF16  BF16 configs only: a_k split into three BF16 planes
  *                               whose sum is a_k exactly (the first two truncate, the

@@ -151,8 +151,10 @@ __global__ __launch_bounds__(256) void derive_kernel(uint8_t* calib, quantwm_cal
       __syncthreads();
     }
     int ek = 0, ev = 0;
-    if (s_max[0][0] > 0.0f) { int x; frexpf(s_max[0][0], &x); ek = x - 15; }  // max in [2^(x-1), 2^x)
-    if (s_max[1][0] > 0.0f) { int x; frexpf(s_max[1][0], &x); ev = x - 15; }
+    // (max in [2^(x-1), 2^x). Not below -109, where BF16's smallest value, 2^-133, becomes
+    // binary16's: smaller tables are exact there as well, and a step times 2^-e stays finite)
+    if (s_max[0][0] > 0.0f) { int x; frexpf(s_max[0][0], &x); ek = max(x - 15, -109); }
+    if (s_max[1][0] > 0.0f) { int x; frexpf(s_max[1][0], &x); ev = max(x - 15, -109); }
     _Float16* __restrict__ hk = reinterpret_cast<_Float16*>(slab + C.mu_k16);
     _Float16* __restrict__ hv = reinterpret_cast<_Float16*>(slab + C.mu_v16);
 #pragma unroll 8

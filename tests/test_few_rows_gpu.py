@@ -173,3 +173,17 @@ def test_large_key_tables(power, small, n_q, few):
         # their weights are equal: half a step of the result, and the sum's order
         err = np.abs(out.double().cpu().numpy() - ref) - 2.0 ** -8 * np.abs(ref) - p.n * 2.0 ** -23 * mag
         assert (err[led.transpose(0, 2, 1)] <= 0).all()
+
+
+@pytest.mark.parametrize("power", [-90, -108, -112, -116, -120])
+@pytest.mark.parametrize("n_q,few", [(1, True), (20, True), (40, False)])
+@pytest.mark.parametrize("steps", [False, True])
+def test_small_value_tables(steps, power, n_q, few):
+    """Value centroids near the smallest normal numbers, and Values that are centroids, or
+    residuals of size 1 upon them."""
+    rng = np.random.default_rng(-power + n_q)
+    n = 7400 if n_q == 20 else 300
+    p = stream(rng, n, **normal(1.0), values=None if steps else members, mu_v=lambda rng, s: 1.0 + np.abs(rng.standard_normal(s)))
+    p.tables = [(t[0], np.ldexp(t[1], power), *t[2:]) for t in p.tables]
+    q = s64.rounded(rng.standard_normal((1, n_q, 2, 128)), "bf16")
+    window(p, q, few)
