@@ -707,6 +707,8 @@ static quantwm_status check_shared(const quantwm_config* prefix_cfg, int64_t n_p
   // Queries and keys are counted in 32 bits, the rollouts' rows together in the prefix pass
   if (n_q > kMaxPositions / cfg->batch || n_prefix > kMaxPositions || n_cache + n_act > kMaxPositions)
     return fail(QWM_ERR_UNSUPPORTED, "more than %lld Queries or keys per head", (long long)kMaxPositions);
+  if (n_q * cfg->batch > qwm::kMaxJoinRows / cfg->heads)
+    return fail(QWM_ERR_UNSUPPORTED, "more than %lld Queries of all heads", (long long)qwm::kMaxJoinRows);
   return QWM_OK;
 }
 

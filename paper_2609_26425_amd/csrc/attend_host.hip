@@ -3,6 +3,7 @@
 // and PSAC rank padding) and the log-sum-exp merge of partial results.
 #include "attend_shape.h"
 #include "few_shape.h"
+#include "grid_rows.h"
 
 namespace qwm {
 namespace {
@@ -79,7 +80,7 @@ __device__ inline JoinRow join_row(const JoinArgs& a, uint32_t row) {
 template <typename T, int D>
 __global__ __launch_bounds__(256) void join_planes(const JoinArgs a) {
   const int64_t rows = int64_t(a.batch) * a.n_q * a.heads;
-  const uint32_t row = blockIdx.x * 4 + threadIdx.x / 64;
+  const uint32_t row = (blockIdx.y * gridDim.x + blockIdx.x) * 4 + threadIdx.x / 64;
   const int lane = threadIdx.x % 64, n = a.n_prefix + a.n_own;
   if (row >= rows) return;
   const JoinRow at = join_row(a, row);
@@ -141,7 +142,7 @@ constexpr int kWidePlanes = 4;
 template <typename T, int D>
 __global__ __launch_bounds__(256) void join_rows(const JoinArgs a) {
   const int64_t rows = int64_t(a.batch) * a.n_q * a.heads;
-  const uint32_t row = blockIdx.x * 16 + threadIdx.x / 16;
+  const uint32_t row = (blockIdx.y * gridDim.x + blockIdx.x) * 16 + threadIdx.x / 16;
   const int l16 = threadIdx.x % 16, n = a.n_prefix + a.n_own;
   if (row >= rows) return;
   const JoinRow at = join_row(a, row);
@@ -188,9 +189,10 @@ hipError_t launch_join_d(const JoinArgs& a, hipStream_t s) {
   // 16 lanes a row from four rows for every SIMD on
   const bool wide = a.n_prefix + a.n_own <= kWidePlanes && rows >= 4096;
   const int64_t wgs = (rows + (wide ? 15 : 3)) / (wide ? 16 : 4);
-  if (rows > 0x7fffffff) return hipErrorInvalidValue;  // (their planes would be 500 GB)
-  if (wide) hipLaunchKernelGGL((join_rows<T, D>), dim3((unsigned)wgs), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((join_planes<T, D>), dim3((unsigned)wgs), dim3(256), 0, s, a);
+  if (rows > kMaxJoinRows) return hipErrorInvalidValue;
+  const dim3 grid(qwm_grid_x(wgs), qwm_grid_y(wgs));
+  if (wide) hipLaunchKernelGGL((join_rows<T, D>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((join_planes<T, D>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -211,6 +211,8 @@ bool attend_few_plan(AttendArgs& a, int batch, int cus, int elem, int most);
 hipError_t launch_attend_few(const AttendArgs& a, int d, int elem, int batch, hipStream_t s, const AttendArgs* other = nullptr,
                              int other_batch = 0);
 bool attend_few_pairs(const quantwm_config& a, const quantwm_config& b);
+// Rows of a join, at most: they are counted in 32 bits.
+constexpr int64_t kMaxJoinRows = 0x7fff0000;
 hipError_t launch_join(const JoinArgs& a, int d, bool bf16_out, hipStream_t s);
 hipError_t launch_rotary(const RotaryArgs& a, int d, bool bf16_data, bool halves, hipStream_t s);
 size_t attend_lds_bytes(int d, int elem, int rank, int n_centroids, bool tables_in_lds);

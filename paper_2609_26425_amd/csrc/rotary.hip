@@ -10,6 +10,7 @@
 // once. Queries and Keys of 4,680 tokens x 40 heads x 128: 192 MB in 31.5 us, 6.1 TB/s
 // with its inputs in part in the caches (a copy of as many bytes: 5.2). A single token's
 // launch is one workgroup: some 6 us from call to end, 2.2 of them the kernel.
+#include "grid_rows.h"
 #include "qwm_common.h"
 
 namespace qwm {
@@ -187,10 +188,8 @@ hipError_t launch_t(const RotaryArgs& a, hipStream_t s) {
   RotaryArgs b = a;
   const int units = a.heads * (D * int(sizeof(T)) / (HALVES ? 32 : 16)), fill = kRotThreads / 2 / units;
   b.block_tokens = fill < 1 ? 1 : (fill < kRotTokens ? fill : kRotTokens);
-  // rows of 2^16 workgroups: a grid dimension holds fewer than 2^32 threads
-  const int64_t wgs = (a.tokens + b.block_tokens - 1) / b.block_tokens, x = wgs < 65536 ? wgs : 65536;
-  hipLaunchKernelGGL((rotary_kernel<T, D, HALVES>), dim3((unsigned)x, (unsigned)((wgs + x - 1) / x)), dim3(kRotThreads), 0, s,
-                     b);
+  const int64_t wgs = (a.tokens + b.block_tokens - 1) / b.block_tokens;
+  hipLaunchKernelGGL((rotary_kernel<T, D, HALVES>), dim3(qwm_grid_x(wgs), qwm_grid_y(wgs)), dim3(kRotThreads), 0, s, b);
   return hipGetLastError();
 }
 
