@@ -357,7 +357,8 @@ size_t quantwm_attend_window_workspace_bytes(const quantwm_config* cfg, int64_t 
  * be NULL. Needs a device workspace of quantwm_attend_shared_workspace_bytes(),
  * 256-byte aligned (QWM_ERR_INVALID_ARG when it is smaller); calls that share one
  * must be ordered on one stream, captured graphs included. QWM_ERR_UNSUPPORTED when
- * B n_q H, n_prefix or n_cache + n_act exceeds 0x7fff0000. */
+ * B n_q H, n_prefix or n_cache + n_act exceeds 0x7fff0000, or, with more Queries than
+ * the few-row kernels take, B or H 65,536. */
 quantwm_status quantwm_attend_shared(const quantwm_config* prefix_cfg, const void* prefix_calibs, int32_t n_epochs,
                                      const int64_t* epoch_start, const void* prefix_cache, int64_t n_prefix,
                                      const quantwm_config* cfg, const void* calib, const void* cache,

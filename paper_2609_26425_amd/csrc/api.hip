@@ -781,6 +781,10 @@ quantwm_status quantwm_attend_shared(const quantwm_config* prefix_cfg, const voi
     few_own = plan(cfg, own, p.few_own, p.own, n_own, static_cast<uint8_t*>(workspace) + p.prefix_bytes);
     c.own_o = own.part_o; c.own_ml = own.part_ml; c.n_own = own.n_split;
   }
+  // heads and rollouts are grid dimensions of the tiled kernel: at most 65,536 (nothing of a call
+  // that one pass cannot take is enqueued)
+  if (((p.prefix > 0 && !few_pre) || (p.own > 0 && !few_own)) && (cfg->heads > 65536 || cfg->batch > 65536))
+    return fail(QWM_ERR_UNSUPPORTED, "more than 65536 heads or rollouts, with more Queries than the few-row kernels take");
   hipError_t e = hipSuccess;
   if (few_pre && few_own && qwm::attend_few_pairs(*prefix_cfg, *cfg)) {
     // chains too short to fill the GPU, side by side (3 rollouts x 33 fp32 Queries over 777

@@ -40,3 +40,11 @@ def test_shared_refuses_more_rows_than_a_join_counts():
     assert size(n_q) > 0 and size(n_q + 1) == 0
     assert _shared(pcfg=pcfg, cfg=cfg, n_q=n_q + 1) == qw.ERR_UNSUPPORTED
     assert "Queries" in qw.quantwm_last_error()
+
+
+def test_shared_refuses_batches_past_the_tiles_grid():
+    """Rollouts and heads are grid dimensions of the tiled kernel (33 Queries and more): refused
+    before the prefix pass is enqueued."""
+    for pcfg, cfg in ((_cfg(heads=1), _cfg(heads=1, batch=70_000)), (_cfg(heads=70_000), _cfg(heads=70_000))):
+        assert _shared(pcfg=pcfg, cfg=cfg, n_q=33, nb=1 << 50) == qw.ERR_UNSUPPORTED
+        assert "65536" in qw.quantwm_last_error()
