@@ -187,3 +187,33 @@ def test_small_value_tables(steps, power, n_q, few):
     p.tables = [(t[0], np.ldexp(t[1], power), *t[2:]) for t in p.tables]
     q = s64.rounded(rng.standard_normal((1, n_q, 2, 128)), "bf16")
     window(p, q, few)
+
+
+# packed, exact keys, Queries, epochs' starts, rank, storage, with a workspace: whether the
+# few-row kernel takes the launch
+LAUNCHES = {
+    "one": (True, 900, 0, 1, [0], 8, 0, True), "one-unsplit": (True, 900, 0, 1, [0], 8, 0, False),
+    "one-of-few-keys": (True, 40, 0, 1, [0], 4, 1, True), "one-act": (True, 900, 70, 1, [0], 0, 0, True),
+    "two-parts-at-least": (False, 900, 70, 1, [0], 0, 0, False), "epochs": (True, 900, 9, 3, [0, 64, 200], 12, 1, True),
+    "many-epochs": (False, 2700, 20, 7, [66 * i for i in range(40)], 4, 0, True),
+    "many-epochs-19": (True, 7200, 20, 19, [180 * i for i in range(40)], 4, 0, True),
+    "sixteen": (True, 5760, 0, 16, [0], 16, 0, True), "sixteen-of-fewer-keys": (False, 5759, 0, 16, [0], 16, 0, True),
+    "wide": (True, 11_904, 0, 32, [0], 4, 0, True), "wide-of-fewer-keys": (False, 11_903, 0, 32, [0], 4, 0, True),
+    "two-blocks": (False, 13_000, 0, 33, [0], 4, 0, True), "odd-rank": (False, 900, 0, 1, [0], 13, 0, True),
+    "even-rank": (False, 900, 0, 1, [0], 6, 1, True),
+}
+
+
+@pytest.mark.parametrize("name", list(LAUNCHES))
+def test_which_kernel_takes_a_launch(name):
+    """Keys around a far point common to all, which cancels in the softmax: rounded to BF16
+    they lose a good part of what tells them apart, so only one of the forms fits the results."""
+    few, n, n_act, n_q, starts, r, st, ws = LAUNCHES[name]
+    rng, H, d = np.random.default_rng(n + n_q + r), 2, 64
+    far = 512.0 * rng.choice([-1.0, 1.0], (H, d))
+    p = stream(rng, n, lambda rng, mk, s: far + 4 * rng.standard_normal(s), lambda rng, s: far[:, None] + 4 * rng.standard_normal(s),
+               starts=starts, heads=H, d=d, kc=16, g=32, r=r, st=st)
+    q = s64.rounded(0.25 * rng.standard_normal((1, n_q, H, d)), "bf16")
+    ka, va = (s64.rounded(x + rng.standard_normal((1, n_act, H, d)), "bf16") if n_act else None for x in (far, 0.0))
+    _, _, either = window(p, q, few, ka, va, ws)
+    assert not either
