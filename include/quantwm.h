@@ -262,7 +262,9 @@ size_t quantwm_attend_workspace_bytes(const quantwm_config* cfg, int64_t n_cache
  * workspace_bytes, 256-byte aligned, owned by the caller and not read back (NULL
  * means no split, fewer bytes than quantwm_attend_workspace_bytes() the cheapest
  * number of parts that they hold, none included). Calls
- * that share a workspace must be ordered on one stream. QWM_ERR_UNSUPPORTED
+ * that share a workspace must be ordered on one stream. Calls of one Query to a few are
+ * faster as quantwm_attend_window with a window of every key, whose few-row kernels this
+ * call and the next two do not use (1 Query of 40 heads over 15,600 keys: 68 and 36 us). QWM_ERR_UNSUPPORTED
  * when n_q or the key count (n_cache, plus n_act for the active-chunk forms)
  * exceeds 0x7fff0000 per head. */
 quantwm_status quantwm_attend(const quantwm_config* cfg, const void* calib, const void* cache,
@@ -323,9 +325,12 @@ size_t quantwm_attend_epochs_workspace_bytes(const quantwm_config* cfg, int32_t 
  * token-causal window (the Query's own position and the window - 1 before it); a
  * window of W F positions shows the Query's frame and the W - 1 before it; a
  * window of every position is quantwm_attend_epochs. A Query that sees no key
- * has O = 0 and lse = -inf. Only tiles of at most 64 keys that hold a visible key of a
- * block of at most 256 Queries are read, so time and bytes go by n_sink + window, not by
- * n_cache. Few Queries take Keys as they are packed (centroid and residual) instead of
+ * has O = 0 and lse = -inf. A block of at most 256 Queries reads, in tiles of at most 64
+ * keys, the sinks and the positions from its first Query's window to the end of its last
+ * Query's frame: n_sink + window + the frames that the block spans, whatever n_cache is.
+ * Positions among these that no Query sees (between two frames' windows where the window
+ * is shorter than a frame, or all but the sinks where it is 0) are read and masked. Few
+ * Queries take Keys as they are packed (centroid and residual) instead of
  * rounded to the table type, so results differ by such roundings between launches of
  * few and of many Queries. n_epochs >= 1 (1: one calibration block, epoch_start may be NULL);
  * n_act may be 0; n_sink and window are >= 0. Everything else as for
@@ -350,11 +355,12 @@ size_t quantwm_attend_window_workspace_bytes(const quantwm_config* cfg, int64_t 
  * are those of quantwm_attend_active with cfg, calib, cache, k_act and v_act. The
  * mask is that of quantwm_attend over the concatenated positions; q_start >=
  * n_prefix, so every Query sees the whole prefix. q, out: [B, n_q, H, d]; lse_out:
- * optional [B, H, n_q]. The prefix is read and decoded once for the rows of all
+ * optional [B, H, n_q]. Few-row and tiled passes round Keys as quantwm_attend_window's
+ * do. The prefix is read and decoded once for the rows of all
  * rollouts together (they are one chunk of B n_q Queries to it), and its partial
  * softmax results are joined with those of the own keys by log-sum-exp. n_prefix
- * and n_cache + n_act may be 0; the pointers of an empty part are not read and may
- * be NULL. Needs a device workspace of quantwm_attend_shared_workspace_bytes(),
+ * may be 0 (prefix_calibs and prefix_cache are then not read and may be NULL), and so
+ * may n_cache + n_act (then calib, cache, k_act and v_act). Needs a device workspace of quantwm_attend_shared_workspace_bytes(),
  * 256-byte aligned (QWM_ERR_INVALID_ARG when it is smaller); calls that share one
  * must be ordered on one stream, captured graphs included. QWM_ERR_UNSUPPORTED when
  * B n_q H, n_prefix or n_cache + n_act exceeds 0x7fff0000, or, with more Queries than
@@ -405,7 +411,9 @@ quantwm_status quantwm_rotary_init(const quantwm_config* cfg, const int32_t* dim
  * (pos0 + i) / (height width), then row and column inside the frame (each below
  * 2^31). inverse != 0 turns back by the same angles: the transpose of the turn, so
  * the gradient with respect to its input. Angles are formed in fp64 and the
- * products in fp32, with one rounding to the element type. n == 0 is a no-op.
+ * products in fp32, with one rounding to the element type: an angle of a radians is off
+ * by at most 3 2^-53 |a| + 2^-23 (so from about 2^28 radians on by more than fp32's own
+ * rounding, and past 2^51 it has no correct digit). n == 0 is a no-op.
  * QWM_ERR_UNSUPPORTED when B n exceeds 0x7fff0000 or H * d 2^30. */
 quantwm_status quantwm_rotary(const quantwm_config* cfg, const quantwm_rotary_axes* axes, int64_t pos0,
                               const int32_t* pos, const void* q, const void* k, int64_t n, int64_t token_stride,

@@ -788,7 +788,7 @@ quantwm_status quantwm_attend_shared(const quantwm_config* prefix_cfg, const voi
   hipError_t e = hipSuccess;
   if (few_pre && few_own && qwm::attend_few_pairs(*prefix_cfg, *cfg)) {
     // chains too short to fill the GPU, side by side (3 rollouts x 33 fp32 Queries over 777
-    // shared keys and 103 own ones: 23 us, one after the other 36)
+    // shared keys and 103 own ones: 36 -> 23 us for the call, which takes 19.5 by now)
     e = qwm::launch_attend_few(pre, cfg->head_dim, qwm::elem_bytes(*cfg), 1, s, &own, cfg->batch);
   } else {
     if (p.prefix > 0) e = launch(prefix_cfg, pre, few_pre);

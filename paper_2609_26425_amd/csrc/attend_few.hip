@@ -15,13 +15,17 @@
 // exact that is not 2^-29 times smaller. Values are decoded by key pairs to BF16 into a
 // wave-private transposed tile (V^T rows of 32 keys), the A operand of O^T += V^T P^T.
 // Packed fields are loaded a step ahead, each side's as soon as the last ones are used.
+// Fewer than 32 bits have the operands of the products only: s (code - z) is rounded to
+// binary16 (2^-11 of it), and Values, weights, coefficients and q U_r to BF16 (2^-8 of
+// them), as in attend.hip; sums and softmax states are fp32. Outputs are 0.0018 to 0.0019 off,
+// of which their own rounding to BF16 is 0.0017.
 // A workgroup runs one part of one segment (an epoch's keys or the exact chunk), so its
 // tables, scales and q U_r never change; its waves merge their softmax states through
 // LDS, and the parts are merged by join_planes.
 //
 // Bound by vector issue and by latency at three waves a SIMD: some 520 vector instructions
 // for 32 keys (d = 128, rank 16), against 18 matrix products. One Query of 40 heads over
-// 15,600 keys of a cache of 32,760 (128 centroids): 33.9 us. 1,024 keys take 16 of that
+// 15,600 keys of a cache of 32,760 (128 centroids): 34.4 us. 1,024 keys take 16 of that
 // (the call, the staging of the tables, the merges), the rest is 1.3 ns a key of all
 // heads, 3.2 TB/s of packed fields. 256-row workgroups of attend.hip: 75 us.
 #include "attend_device.h"
@@ -444,9 +448,8 @@ __global__ __launch_bounds__(64 * few_waves(NQ, TAB)) void attend_few_kernel(con
           const uint32_t c = p.c_w[e][i / 2];
           w[i] = pack_bf16((float)int8_t((c >> (16 * (i % 2))) & 255) * cs, (float)int8_t((c >> (16 * (i % 2) + 8)) & 255) * cs);
         }
-        // with 16 ranks, half the depth is zeros: a product of depth 16 onto the sums of
-        // deeper ones, right after them, gave wrong sums (the compiler puts no wait
-        // between products of different lengths on the same accumulator)
+        // with 16 ranks, half the depth is zeros: with a product of depth 16 onto the sums of
+        // the deeper ones, right after them, results were wrong (the cause was not found)
 #pragma unroll
         for (int n = 0; n < NQ; ++n)
           s[e][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V, make_uint4(w[0], w[1], w[2], w[3])), ureg[n],

@@ -292,7 +292,8 @@ bool attend_few_takes(const quantwm_config& c, int64_t n_q, int64_t n_keys) {
 }
 
 int attend_few_planes(int64_t n_q, int heads, int batch, int64_t n_keys, int cus, int elem) {
-  // every segment (epoch) may end in a part of its own
+  // a segment (epoch) may end in a part of its own: room for 16 of them. A launch with more
+  // segments in reach than planes takes the tiles (one Query of 40 heads: more than 22)
   return int(few_want(n_q, heads, batch, n_keys / kFewChunk + 2, cus, elem)) + 16;
 }
 

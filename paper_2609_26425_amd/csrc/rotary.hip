@@ -5,8 +5,9 @@
 // a few whole tokens, computes their cosines and sines once into LDS, and turns
 // every head of the Queries and the Keys with them. A far position's angle needs
 // more than fp32: turns = x f / 2 pi is formed and reduced to [-1/2, 1/2] in fp64,
-// and only the remainder goes to fp32 (2^-25 of a turn), so the cosines are right
-// to fp32 for any position. Memory bound: every value is read once and written
+// and only the remainder goes to fp32. That is off by three roundings of the whole angle
+// (2 pi, f / 2 pi and the product: at most 3 2^-53 of it) and by 2^-26 of a turn: some
+// 1e-7 radians in all up to angles of 2^27, 8e-7 at position 2^31 with f = 1. Memory bound: every value is read once and written
 // once. Queries and Keys of 4,680 tokens x 40 heads x 128: 192 MB in 31.5 us, 6.1 TB/s
 // with its inputs in part in the caches (a copy of as many bytes: 5.2). A single token's
 // launch is one workgroup: some 6 us from call to end, 2.2 of them the kernel.
