@@ -23,9 +23,9 @@
 // tables, scales and q U_r never change; its waves merge their softmax states through
 // LDS, and the parts are merged by join_planes.
 //
-// Bound by vector issue and by latency at three waves a SIMD: some 520 vector instructions
+// Bound by vector issue and by latency at three waves a SIMD: some 530 vector instructions
 // for 32 keys (d = 128, rank 16), against 18 matrix products. One Query of 40 heads over
-// 15,600 keys of a cache of 32,760 (128 centroids): 34.4 us. 1,024 keys take 16 of that
+// 15,600 keys of a cache of 32,760 (128 centroids): 34.6 us. 1,024 keys take 16 of that
 // (the call, the staging of the tables, the merges), the rest is 1.3 ns a key of all
 // heads, 3.2 TB/s of packed fields. 256-row workgroups of attend.hip: 75 us.
 #include "attend_device.h"
